@@ -9,7 +9,8 @@
  * block list (Section 3.3.2: iteration time grows with the tokens in the
  * batch), and every preemption by swapping (Section 2.5, Section 3.5: cost
  * linear in sequence length) or KV reuse is a copy of KV blocks.  This library
- * is those two operations and nothing else.
+ * is those two operations and what keeps the blocks around them: tables and slots for
+ * new tokens, the writes, bounds of each block's keys, and attention over a part of the blocks.
  *
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE memory owned by the caller unless a comment
@@ -329,6 +330,115 @@ KVC_API int kvc_kv_block_copy(const kvc_pool *src, const kvc_pool *dst, const in
  * memory (KVC_ERR_OVERLAP). */
 KVC_API int kvc_validate_block_mapping(const kvc_pool *src, const kvc_pool *dst,
                                const int64_t *block_mapping, int64_t num_pairs, void *hip_stream);
+
+/*
+ * ---- Block tables, writes of many tokens, and attention over a part of the blocks
+ *
+ * The calls below read these fields of the descriptor: num_seqs, num_q_heads, num_kv_heads, head_dim, block_size,
+ * max_blocks_per_seq, num_pool_blocks, dtype and max_context_len; partition_tokens and kernel are ignored.
+ */
+
+/* Where kvc_block_tables_extend writes (host struct of device pointers, read during the call).  "may be NULL": not written. */
+typedef struct {
+    int32_t *q_start;      /* [num_seqs + 1] first row of each sequence's new tokens, as kvc_paged_attention_prefill takes it */
+    int32_t *context_lens; /* [num_seqs] tokens after the call */
+    int32_t *held_blocks;  /* [num_seqs] blocks after the call; may be NULL */
+    int32_t *taken;        /* [1] blocks taken off the front of free_blocks; may be NULL */
+    int64_t *slot_map;     /* [max_rows] block * block_size + slot of every new token, -1 behind the last row */
+    int32_t *positions;    /* [max_rows] position of every new token in its sequence, -1 behind; may be NULL */
+    int32_t *row_seqs;     /* [max_rows] sequence of every new token, -1 behind; may be NULL */
+    int32_t max_rows;      /* rows the maps have room for, below 2^31 - 1 */
+    int32_t reserved;      /* must be 0 */
+} kvc_table_update;
+
+/*
+ * Room for the new tokens of an iteration: every sequence gets the blocks that its new tokens lack from the front of a free
+ * list, in the order of the batch, and every new token its slot (block-based allocation: Section 1, Section 3.3).
+ *   block_tables   int32 [num_seqs][max_blocks_per_seq]: entries held .. ceil((ctx + new) / block_size) - 1 of a sequence that
+ *                  gets blocks are written, all others left as they are
+ *   context_lens   int32 [num_seqs]: tokens each sequence has;   new_lens   int32 [num_seqs]: tokens to add (0 and below: none)
+ *   held_blocks    int32 [num_seqs]: entries of each table row that name blocks already (a request may hold more than its
+ *                  tokens fill); NULL: ceil(context_len / block_size)
+ *   free_blocks    int32 [num_free], num_free below 2^31 - 1; may be NULL when num_free is 0
+ * A sequence gets all it asks for or nothing.  It gets nothing, brings no rows (its q_start entries are equal) and keeps its
+ * length and blocks when
+ *   - its lengths or held blocks are negative or past its table, or its new tokens do not fit the table;
+ *   - it lacks blocks and they, with those that the sequences before it ask for (granted or not), exceed num_free;
+ *   - its new tokens, with those of the sequences before it (granted or not), exceed max_rows.
+ * The sequences behind go by the same rules, so what is taken is always the front of free_blocks.  A new token whose table
+ * entry is negative gets slot -1.  No output may overlap another array of the call (KVC_ERR_OVERLAP).  Up to 4096 sequences one launch,
+ * above two.  With num_seqs == 0 the maps are filled with -1.
+ */
+KVC_API int kvc_block_tables_extend(int32_t *block_tables, const int32_t *context_lens, const int32_t *new_lens,
+                                    const int32_t *held_blocks, const int32_t *free_blocks, int32_t num_free,
+                                    const kvc_table_update *update, const kvc_attn_desc *desc, void *hip_stream);
+
+/*
+ * K and V of many new tokens into their slots (kvc_kv_cache_append for any number of tokens per sequence).
+ *   k_new, v_new   T [num_rows][num_kv_heads][head_dim], 16-byte aligned; consecutive rows lie k_row_stride / v_row_stride
+ *                  elements apart (0: packed; at least num_kv_heads * head_dim, a multiple of 16 bytes), so that a fused
+ *                  projection's output can be passed as it is
+ *   slot_map       int64 [num_rows]: block * block_size + slot; a row whose slot is negative, or at or past
+ *                  num_pool_blocks * block_size, is not written
+ * Every other byte of the caches is left untouched.  A slot should appear once: of two rows with the same slot either may
+ * win, word by word.
+ */
+KVC_API int kvc_kv_cache_write(const void *k_new, const void *v_new, int64_t k_row_stride, int64_t v_row_stride, void *k_cache,
+                               void *v_cache, const int64_t *slot_map, int32_t num_rows, const kvc_attn_desc *desc,
+                               void *hip_stream);
+
+/*
+ * Bounds of the keys of every block that new tokens filled:
+ *   bounds   T [num_pool_blocks][num_kv_heads][2][head_dim]: per channel the smallest (0) and the largest (1) key of the block's
+ *            block_size tokens, NaN where one is NaN.  16-byte aligned.
+ *   context_lens   tokens of each sequence after the new ones;  q_start as in kvc_paged_attention_prefill, NULL: one new token
+ *            per sequence.  max_query_len: host-known bound on the new tokens of a sequence (1 without q_start).
+ * Blocks floor((S - Q) / block_size) .. floor(S / block_size) - 1 of a sequence of S tokens, Q of them new, are computed from
+ * the cache (blocks of tokens past a sequence's first max_query_len new ones may be left out); all others are left as they
+ * are.  To rebuild the bounds of whole sequences (after a swap-in) pass all their tokens as new.  Table entries outside the
+ * pool are passed over.
+ */
+KVC_API int kvc_key_bounds_update(const void *k_cache, void *bounds, const int32_t *block_tables, const int32_t *context_lens,
+                                  const int32_t *q_start, const kvc_attn_desc *desc, int32_t max_query_len, void *hip_stream);
+
+/*
+ * The blocks that each query keeps.  Row i of q belongs to the sequence and stands at the position that
+ * kvc_paged_attention_prefill gives it; with q_start == NULL row n is the last position of sequence n (a decode step,
+ * total_q == num_seqs).  A row at position p sees nb = floor(p / block_size) + 1 blocks.
+ *   selected   int32 [total_q][num_kv_heads][budget]: places in the row's block table, ascending, -1 behind them.
+ * nb <= budget: all of them.  Otherwise the first keep_first (>= 0) and the last keep_last (>= 1) blocks, which are always
+ * kept, and of the others the budget - keep_first - keep_last of largest
+ *   score(b) = max over the heads h of the KV head's group of sum_d max(q[h][d] * bounds[b][0][d], q[h][d] * bounds[b][1][d]),
+ * which no product of a head's query with a key of the block exceeds.  Scores are computed in 64 bits; of equal ones the
+ * lower block is kept; a score that is not finite (something in the bounds or the query is not) ranks above all others.  Only blocks
+ * before the row's own are scored, so bounds of full blocks are all that is read.
+ *   - Rows that belong to no sequence (before q_start[0], at or past q_start[num_seqs]) are left as they were; a row of a
+ *     sequence without tokens gets -1 throughout.
+ *   - Positions at or past max_context_len are taken for the last one below it.
+ *   - workspace: device memory, 256-byte aligned, kvc_block_select_workspace_bytes(desc, total_q, ...) of it (may be NULL when
+ *     that is 0): scratch, needs no preparation.  Calls that share one must not overlap in time.
+ */
+KVC_API size_t kvc_block_select_workspace_bytes(const kvc_attn_desc *desc, int32_t total_q, int32_t budget, int32_t keep_first,
+                                                int32_t keep_last);
+KVC_API int kvc_block_select(const void *q, const void *bounds, const int32_t *block_tables, const int32_t *context_lens,
+                             const int32_t *q_start, int32_t *selected, int32_t budget, int32_t keep_first, int32_t keep_last,
+                             const kvc_attn_desc *desc, int32_t total_q, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Attention of each query over the blocks it keeps:
+ *   out[i][h][:] = sum_t softmax_t( scale * q[i][h] . K[t] ) * V[t] over the tokens t <= position of row i that lie in a block of
+ *   selected[i][h / group][:] (int32 [total_q][num_kv_heads][budget]).
+ * Rows, positions and q_start as in kvc_block_select.  A list may be in any order; entries below 0 or past the row's own block are
+ * passed over; an entry that appears twice counts twice.  A row whose list leaves nothing gets zeros; rows that belong to no
+ * sequence are left as they were.  Accumulation is fp32, output rounded to nearest even.
+ *   - workspace: device memory, 256-byte aligned, kvc_paged_attention_selected_workspace_bytes(desc, total_q, budget) of it
+ *     (may be NULL when that is 0): scratch, needs no preparation.  Calls that share one must not overlap in time.
+ */
+KVC_API size_t kvc_paged_attention_selected_workspace_bytes(const kvc_attn_desc *desc, int32_t total_q, int32_t budget);
+KVC_API int kvc_paged_attention_selected(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables,
+                                         const int32_t *context_lens, const int32_t *q_start, const int32_t *selected, int32_t budget,
+                                         float scale, void *out, const kvc_attn_desc *desc, int32_t total_q, void *workspace,
+                                         size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

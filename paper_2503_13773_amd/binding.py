@@ -1,9 +1,10 @@
 """ctypes binding of the C ABI in include/kvc.h (same names, argument marshalling only)."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch  # device memory and streams; also makes sure one HIP runtime is shared
 
@@ -95,6 +96,17 @@ def lib():
     L.kvc_kv_block_copy.argtypes = [pp, pp, vp, ctypes.c_int64, vp]
     L.kvc_validate_block_mapping.restype = ctypes.c_int
     L.kvc_validate_block_mapping.argtypes = [pp, pp, vp, ctypes.c_int64, vp]
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    for name, result, args in (
+            ("kvc_block_tables_extend", ctypes.c_int, [vp, i32p, i32p, i32p, i32p, i32, ctypes.POINTER(TableUpdateArgs), dp, vp]),
+            ("kvc_kv_cache_write", ctypes.c_int, [vp, vp, i64, i64, vp, vp, vp, i32, dp, vp]),
+            ("kvc_key_bounds_update", ctypes.c_int, [vp, vp, i32p, i32p, i32p, dp, i32, vp]),
+            ("kvc_block_select_workspace_bytes", sz, [dp, i32, i32, i32, i32]),
+            ("kvc_block_select", ctypes.c_int, [vp, vp, i32p, i32p, i32p, i32p, i32, i32, i32, dp, i32, vp, sz, vp]),
+            ("kvc_paged_attention_selected_workspace_bytes", sz, [dp, i32, i32]),
+            ("kvc_paged_attention_selected", ctypes.c_int, [vp, vp, vp, i32p, i32p, i32p, i32p, i32, f, vp, dp, i32, vp, sz, vp])):
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = result, args
     _lib = L
     return L
 
@@ -457,3 +469,241 @@ def validate_block_mapping(src_pool, dst_pool, block_mapping, stream=None) -> in
     n = block_mapping.numel() // 2
     return int(lib().kvc_validate_block_mapping(ctypes.byref(src), ctypes.byref(dst),
                                                 block_mapping.data_ptr(), n, _stream_handle(stream)))
+
+
+# ---- operators around the cache's blocks
+
+class TableUpdateArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q_start", "context_lens", "held_blocks", "taken", "slot_map", "positions",
+                                               "row_seqs")] + [("max_rows", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class TableUpdate(NamedTuple):
+    """What block_tables_extend writes: q_start [num_seqs + 1], context_lens and held_blocks [num_seqs], taken [1], and per
+    row slot_map (int64), positions and row_seqs; -1 behind the last row."""
+    q_start: torch.Tensor
+    context_lens: torch.Tensor
+    held_blocks: torch.Tensor
+    taken: torch.Tensor
+    slot_map: torch.Tensor
+    positions: torch.Tensor
+    row_seqs: torch.Tensor
+
+
+def _on_stream(stream):
+    """Allocations of a call belong to the stream that it works on."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def _require_together(*tensors) -> None:
+    """Contiguous tensors on the current device (None: left out)."""
+    for t in tensors:
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+            raise ValueError("tensors must be contiguous device tensors")
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError("tensors must be on the current device")
+
+
+def _require_int32(**tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.dtype != torch.int32:
+            raise TypeError(f"{name} must be int32")
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def new_table_update(num_seqs: int, max_rows: int, device="cuda") -> TableUpdate:
+    def ints(n, dtype=torch.int32):
+        return torch.empty(n, dtype=dtype, device=device)
+    return TableUpdate(ints(num_seqs + 1), ints(num_seqs), ints(num_seqs), ints(1), ints(max_rows, torch.int64), ints(max_rows),
+                       ints(max_rows))
+
+
+def block_tables_extend(block_tables, context_lens, new_lens, free_blocks, block_size: int, *, max_rows: Optional[int] = None,
+                        held_blocks=None, out: Optional[TableUpdate] = None, stream=None) -> TableUpdate:
+    """Blocks from the front of free_blocks for new_lens[n] more tokens of every sequence (written into block_tables), and the
+    slot, position and sequence of every new token.  A sequence gets all it asks for or nothing (see include/kvc.h)."""
+    if out is None and max_rows is None:
+        raise ValueError("max_rows or out is required")
+    if out is None:
+        with _on_stream(stream):
+            out = new_table_update(context_lens.shape[0], int(max_rows), block_tables.device)
+    _require_together(block_tables, context_lens, new_lens, held_blocks, free_blocks, *out)
+    _require_int32(block_tables=block_tables, context_lens=context_lens, new_lens=new_lens, held_blocks=held_blocks,
+                   free_blocks=free_blocks, **{"out." + n: t for n, t in out._asdict().items() if n != "slot_map"})
+    if out.slot_map.dtype != torch.int64:
+        raise TypeError("slot_map must be int64")
+    n = context_lens.shape[0] if context_lens.dim() == 1 else -1
+    if block_tables.dim() != 2 or block_tables.shape[0] != n or new_lens.shape != (n,) or free_blocks.dim() != 1 \
+            or (held_blocks is not None and held_blocks.shape != (n,)):
+        raise ValueError("block_tables, context_lens, new_lens, held_blocks and free_blocks do not match")
+    rows = out.slot_map.shape[0]
+    if out.q_start.shape != (n + 1,) or out.context_lens.shape != (n,) or out.held_blocks.shape != (n,) or out.taken.shape != (1,) \
+            or any(t.shape != (rows,) for t in (out.slot_map, out.positions, out.row_seqs)) or max_rows not in (None, rows):
+        raise ValueError("out does not match the batch")
+    desc = AttnDesc(num_seqs=n, num_q_heads=1, num_kv_heads=1, head_dim=64, block_size=int(block_size),
+                    max_blocks_per_seq=block_tables.shape[1], num_pool_blocks=1, dtype=KVC_BF16)
+    args = TableUpdateArgs(*(_ptr(t) for t in out), max_rows=rows, reserved=0)
+    _check(lib().kvc_block_tables_extend(
+        block_tables.data_ptr(), context_lens.data_ptr(), new_lens.data_ptr(), _ptr(held_blocks), free_blocks.data_ptr(),
+        free_blocks.shape[0], ctypes.byref(args), ctypes.byref(desc), _stream_handle(stream)), "kvc_block_tables_extend")
+    return out
+
+
+def _row_stride(t) -> int:
+    """Elements between the rows of [rows][heads][head_dim], whose rows themselves are packed."""
+    if t.dim() != 3 or (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
+        raise ValueError("rows of k_new / v_new must be packed [num_kv_heads][head_dim]")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1] * t.shape[2]:
+        raise ValueError("rows of k_new / v_new must not overlap")
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def kv_cache_write(k_new, v_new, k_cache, v_cache, slot_map, stream=None) -> None:
+    """Rows k_new[i], v_new[i] ([rows][num_kv_heads][head_dim]; rows may lie apart, as views into a fused projection do) to slot
+    slot_map[i] = block * block_size + slot of the caches; a slot outside the pool skips the row."""
+    _require_together(k_cache, v_cache, slot_map)
+    ks, vs = _row_stride(k_new), _row_stride(v_new)
+    if not (k_new.is_cuda and v_new.is_cuda and k_new.device == v_new.device == k_cache.device):
+        raise ValueError("tensors must be on the current device")
+    rows, hkv, d = k_new.shape
+    if v_new.shape != k_new.shape or k_cache.dim() != 4 or v_cache.shape != k_cache.shape or k_cache.shape[1] != hkv \
+            or k_cache.shape[3] != d or not (k_new.dtype == v_new.dtype == k_cache.dtype == v_cache.dtype):
+        raise ValueError("k_new / v_new / caches do not match")
+    if slot_map.dtype != torch.int64 or slot_map.shape != (rows,):
+        raise TypeError("slot_map must be int64 [rows]")
+    desc = AttnDesc(num_seqs=0, num_q_heads=hkv, num_kv_heads=hkv, head_dim=d, block_size=k_cache.shape[2], max_blocks_per_seq=1,
+                    num_pool_blocks=k_cache.shape[0], dtype=_dtype_code(k_new))
+    _check(lib().kvc_kv_cache_write(k_new.data_ptr(), v_new.data_ptr(), ks, vs, k_cache.data_ptr(), v_cache.data_ptr(),
+                                    slot_map.data_ptr(), rows, ctypes.byref(desc), _stream_handle(stream)), "kvc_kv_cache_write")
+
+
+def new_key_bounds(k_cache):
+    """Bounds for every block of a cache [blocks][num_kv_heads][block_size][head_dim], to be filled by key_bounds_update."""
+    nb, hkv, _, d = k_cache.shape
+    return torch.zeros((nb, hkv, 2, d), dtype=k_cache.dtype, device=k_cache.device)
+
+
+def _check_batch(block_tables, context_lens, q_start) -> None:
+    _require_int32(block_tables=block_tables, context_lens=context_lens, q_start=q_start)
+    if block_tables.dim() != 2 or context_lens.shape != block_tables.shape[:1] \
+            or (q_start is not None and q_start.shape != (block_tables.shape[0] + 1,)):
+        raise ValueError("block_tables, context_lens and q_start do not match")
+
+
+def key_bounds_update(k_cache, bounds, block_tables, context_lens, q_start=None, max_query_len: int = 1, stream=None) -> None:
+    """Smallest and largest key per channel of every block that the new tokens filled: the last q_start[n+1] - q_start[n] of the
+    context_lens[n] tokens of sequence n, or the last one without q_start."""
+    _require_together(k_cache, bounds, block_tables, context_lens, q_start)
+    _check_batch(block_tables, context_lens, q_start)
+    if k_cache.dim() != 4 or bounds.dtype != k_cache.dtype:
+        raise ValueError("bounds and k_cache do not match")
+    nb, hkv, bs, d = k_cache.shape
+    if bounds.shape != (nb, hkv, 2, d):
+        raise ValueError("bounds must be [blocks][num_kv_heads][2][head_dim]")
+    desc = AttnDesc(num_seqs=block_tables.shape[0], num_q_heads=hkv, num_kv_heads=hkv, head_dim=d, block_size=bs,
+                    max_blocks_per_seq=block_tables.shape[1], num_pool_blocks=nb, dtype=_dtype_code(k_cache))
+    _check(lib().kvc_key_bounds_update(k_cache.data_ptr(), bounds.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
+                                       _ptr(q_start), ctypes.byref(desc), int(max_query_len), _stream_handle(stream)),
+           "kvc_key_bounds_update")
+
+
+def _rows_desc(q, blocks, hkv, block_size, block_tables, max_context_len) -> AttnDesc:
+    return AttnDesc(num_seqs=block_tables.shape[0], num_q_heads=q.shape[1], num_kv_heads=hkv, head_dim=q.shape[2],
+                    block_size=int(block_size), max_blocks_per_seq=block_tables.shape[1], num_pool_blocks=blocks,
+                    dtype=_dtype_code(q), max_context_len=int(max_context_len))
+
+
+def _select_desc(q, bounds, block_tables, block_size, max_context_len) -> AttnDesc:
+    if q.dim() != 3 or bounds.dim() != 4 or bounds.shape[2] != 2 or bounds.shape[3] != q.shape[2] or bounds.dtype != q.dtype \
+            or block_tables.dim() != 2:
+        raise ValueError("q, bounds and block_tables do not match")
+    return _rows_desc(q, bounds.shape[0], bounds.shape[1], block_size, block_tables, max_context_len)
+
+
+def _workspace_of(need: int, device, stream=None):
+    if not need:
+        return None
+    with _on_stream(stream):
+        return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+def _workspace_arg(workspace):
+    if workspace is None:
+        return None, 0
+    _require_together(workspace)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def new_select_workspace(q, bounds, block_tables, budget: int, *, block_size: int, max_context_len: int = 0):
+    """A workspace for block_select of these shapes (None when it needs none)."""
+    desc = _select_desc(q, bounds, block_tables, block_size, max_context_len)
+    return _workspace_of(int(lib().kvc_block_select_workspace_bytes(ctypes.byref(desc), q.shape[0], int(budget), 0, 1)), q.device)
+
+
+def block_select(q, bounds, block_tables, context_lens, budget: int, *, block_size: int, keep_first: int = 1, keep_last: int = 1,
+                 q_start=None, max_context_len: int = 0, out=None, workspace=None, stream=None):
+    """The blocks that each query keeps, per KV head: int32 [rows][num_kv_heads][budget], places in the row's block table in
+    ascending order, -1 behind them.  The first keep_first and the last keep_last blocks always, the others by the largest
+    product that a key inside the block's bounds can have with the query."""
+    desc = _select_desc(q, bounds, block_tables, block_size, max_context_len)
+    _check_batch(block_tables, context_lens, q_start)
+    shape = (q.shape[0], bounds.shape[1], int(budget))
+    if out is None:
+        with _on_stream(stream):
+            out = torch.full(shape, -1, dtype=torch.int32, device=q.device)
+    if out.shape != shape or out.dtype != torch.int32:
+        raise ValueError("out must be int32 [rows][num_kv_heads][budget]")
+    _require_together(q, bounds, block_tables, context_lens, q_start, out)
+    if workspace is None:
+        workspace = _workspace_of(int(lib().kvc_block_select_workspace_bytes(ctypes.byref(desc), q.shape[0], int(budget),
+                                                                             int(keep_first), int(keep_last))), q.device, stream)
+    ws, ws_bytes = _workspace_arg(workspace)
+    _check(lib().kvc_block_select(q.data_ptr(), bounds.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(), _ptr(q_start),
+                                  out.data_ptr(), int(budget), int(keep_first), int(keep_last), ctypes.byref(desc), q.shape[0],
+                                  ws, ws_bytes, _stream_handle(stream)), "kvc_block_select")
+    return out
+
+
+def _selected_desc(q, k_cache, block_tables, max_context_len) -> AttnDesc:
+    if q.dim() != 3 or k_cache.dim() != 4 or k_cache.shape[3] != q.shape[2] or k_cache.dtype != q.dtype or block_tables.dim() != 2:
+        raise ValueError("q, k_cache and block_tables do not match")
+    return _rows_desc(q, k_cache.shape[0], k_cache.shape[1], k_cache.shape[2], block_tables, max_context_len)
+
+
+def new_selected_workspace(q, k_cache, block_tables, budget: int, *, max_context_len: int = 0):
+    """A workspace for paged_attention_selected of these shapes (None when it needs none)."""
+    desc = _selected_desc(q, k_cache, block_tables, max_context_len)
+    return _workspace_of(int(lib().kvc_paged_attention_selected_workspace_bytes(ctypes.byref(desc), q.shape[0], int(budget))),
+                         q.device)
+
+
+def paged_attention_selected(q, k_cache, v_cache, block_tables, context_lens, selected, scale: float, *, q_start=None, out=None,
+                             max_context_len: int = 0, workspace=None, stream=None):
+    """out[i,h] = softmax(scale * q[i,h] . K) V over the tokens up to row i's position in the blocks selected[i, h's KV head]."""
+    desc = _selected_desc(q, k_cache, block_tables, max_context_len)
+    _check_batch(block_tables, context_lens, q_start)
+    if v_cache.shape != k_cache.shape or v_cache.dtype != q.dtype:
+        raise ValueError("k_cache / v_cache must match each other and q's dtype")
+    if selected.dtype != torch.int32 or selected.dim() != 3 or selected.shape[:2] != (q.shape[0], k_cache.shape[1]):
+        raise ValueError("selected must be int32 [rows][num_kv_heads][budget]")
+    if out is None:
+        with _on_stream(stream):
+            out = torch.zeros_like(q)
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must look like q")
+    _require_together(q, k_cache, v_cache, block_tables, context_lens, q_start, selected, out)
+    budget = selected.shape[2]
+    if workspace is None:
+        workspace = _workspace_of(int(lib().kvc_paged_attention_selected_workspace_bytes(ctypes.byref(desc), q.shape[0], budget)),
+                                  q.device, stream)
+    ws, ws_bytes = _workspace_arg(workspace)
+    _check(lib().kvc_paged_attention_selected(
+        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(), _ptr(q_start),
+        selected.data_ptr(), budget, float(scale), out.data_ptr(), ctypes.byref(desc), q.shape[0], ws, ws_bytes,
+        _stream_handle(stream)), "kvc_paged_attention_selected")
+    return out

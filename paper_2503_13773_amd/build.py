@@ -17,7 +17,8 @@ SOURCES = ["kvc_api.hip", "kv_block_copy.hip", "kv_cache_append.hip", "paged_att
            "paged_attention_mfma.hip", "paged_attention_mfma_stream.hip", "paged_attention_mfma_rows.hip", "paged_attention_prefill.hip", "paged_attention_prefill32.hip",
            "paged_attention_prefill_wide.hip",
            "paged_attention_prefill_d64.hip",
-           "paged_attention_merge.hip"]
+           "paged_attention_merge.hip", "block_tables.hip", "kv_cache_write.hip", "key_bounds.hip", "block_select.hip",
+           "paged_attention_selected.hip"]
 # packed-fp32 instructions are switched off on purpose for this target
 # The atomic optimizer is switched off: it rewrites an atomic add issued by one lane into a
 # wavefront-wide reduction that reads the result back at once, which makes the balanced

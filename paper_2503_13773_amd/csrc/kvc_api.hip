@@ -214,7 +214,8 @@ int64_t few_row_parts(const kvc_attn_desc &d, int heads, int64_t parts) {
     return d.dtype == KVC_BF16 && wide_rows && d.num_q_heads == 4 * d.num_kv_heads && parts > 1 ? 320 : 384;
 }
 
-int make_plan(const kvc_attn_desc *d, Plan *pl) {
+// What every call asks of a descriptor.
+int check_desc(const kvc_attn_desc *d) {
     if (!d) return KVC_ERR_NULL;
     if (d->num_seqs < 0 || d->num_q_heads <= 0 || d->num_kv_heads <= 0 || d->head_dim <= 0 ||
         d->block_size <= 0 || d->max_blocks_per_seq <= 0 || d->num_pool_blocks <= 0 ||
@@ -227,7 +228,39 @@ int make_plan(const kvc_attn_desc *d, Plan *pl) {
     const int64_t table_tokens = int64_t(d->max_blocks_per_seq) * d->block_size;
     if (table_tokens > 0x40000000) return KVC_ERR_BAD_SHAPE;
     if (d->max_context_len > table_tokens) return KVC_ERR_BAD_SHAPE;
-    const int max_ctx = d->max_context_len ? d->max_context_len : int(table_tokens);
+    return KVC_OK;
+}
+// Tokens that no context of a descriptor has more of.
+int bound_of(const kvc_attn_desc &d) { return d.max_context_len ? d.max_context_len : d.max_blocks_per_seq * d.block_size; }
+
+// A descriptor and the rows of a call with a workgroup or more per (row, KV head): HIP refuses 2^32 threads and more.
+int check_rows(const kvc_attn_desc *d, int32_t total_q) {
+    const int rc = check_desc(d);
+    if (rc != KVC_OK) return rc;
+    const int64_t chunks = d->num_q_heads / d->num_kv_heads;
+    return total_q < 0 || int64_t(total_q) * d->num_kv_heads >= (int64_t(1) << 32) / kvc::kThreads || chunks > 65535 ? KVC_ERR_BAD_SHAPE : KVC_OK;
+}
+
+int select_args(const kvc_attn_desc *d, int32_t total_q, int32_t budget, int32_t keep_first, int32_t keep_last, kvc::SelectArgs *a) {
+    const int rc = check_rows(d, total_q);
+    if (rc != KVC_OK) return rc;
+    // the row's own block, which may not be full yet, is always kept
+    if (budget <= 0 || keep_first < 0 || keep_last < 1 || int64_t(keep_first) + keep_last > budget) return KVC_ERR_BAD_SHAPE;
+    const int bound = bound_of(*d);
+    *a = {d->num_seqs, d->num_q_heads, d->num_kv_heads, d->num_q_heads / d->num_kv_heads, ilog2(d->block_size), d->max_blocks_per_seq, bound,
+          int(ceil_div(bound, d->block_size)), budget, keep_first, keep_last};
+    return KVC_OK;
+}
+// A key for every block that a row can see, unless none competes.
+size_t select_bytes(const kvc::SelectArgs &a, int32_t total_q) {
+    if (a.max_blocks <= a.budget || a.budget == a.keep_first + a.keep_last) return 0;
+    return size_t(total_q) * a.num_kv_heads * a.max_blocks * sizeof(uint64_t);
+}
+
+int make_plan(const kvc_attn_desc *d, Plan *pl) {
+    const int rc = check_desc(d);
+    if (rc != KVC_OK) return rc;
+    const int max_ctx = bound_of(*d);
     if (d->partition_tokens % 16 != 0) return KVC_ERR_BAD_SHAPE;
     if (d->partition_tokens > (d->kernel == KVC_KERNEL_MFMA_BALANCED ? kMaxBalancedChunkTokens : kMaxPartitionTokens))
         return KVC_ERR_BAD_SHAPE;
@@ -813,6 +846,124 @@ int kvc_validate_block_mapping(const kvc_pool *src, const kvc_pool *dst,
             if (std::binary_search(dsts.begin(), dsts.end(), s)) return KVC_ERR_OVERLAP;
     }
     return KVC_OK;
+}
+
+// ---- operators around the cache's blocks
+
+int kvc_block_tables_extend(int32_t *block_tables, const int32_t *context_lens, const int32_t *new_lens, const int32_t *held_blocks,
+                            const int32_t *free_blocks, int32_t num_free, const kvc_table_update *update, const kvc_attn_desc *desc,
+                            void *hip_stream) {
+    const int rc = check_desc(desc);
+    if (rc != KVC_OK) return rc;
+    if (!update) return KVC_ERR_NULL;
+    // sums over the batch stop at 2^31 - 1
+    if (num_free < 0 || num_free == INT32_MAX || update->max_rows < 0 || update->max_rows == INT32_MAX || update->reserved != 0)
+        return KVC_ERR_BAD_SHAPE;
+    if (!update->q_start || (update->max_rows > 0 && !update->slot_map) || (num_free > 0 && !free_blocks)) return KVC_ERR_NULL;
+    if (desc->num_seqs > 0 && (!block_tables || !context_lens || !new_lens || !update->context_lens)) return KVC_ERR_NULL;
+    const int64_t n = desc->num_seqs, rows = update->max_rows, table = n * desc->max_blocks_per_seq;
+    const struct Range { const void *at; int64_t bytes; } ranges[] = {
+        {update->q_start, 4 * (n + 1)}, {update->context_lens, 4 * n}, {update->held_blocks, 4 * n}, {update->taken, 4},
+        {update->slot_map, 8 * rows}, {update->positions, 4 * rows}, {update->row_seqs, 4 * rows}, {block_tables, 4 * table},
+        {context_lens, 4 * n}, {new_lens, 4 * n}, {held_blocks, 4 * n}, {free_blocks, 4 * int64_t(num_free)}};
+    constexpr int kOutputs = 8;  // the first ones
+    for (int i = 0; i < kOutputs; ++i)
+        for (int j = i + 1; j < int(sizeof ranges / sizeof *ranges); ++j) {
+            const uintptr_t x = reinterpret_cast<uintptr_t>(ranges[i].at), y = reinterpret_cast<uintptr_t>(ranges[j].at);
+            if (x && y && ranges[i].bytes > 0 && ranges[j].bytes > 0 && x < y + uintptr_t(ranges[j].bytes) && y < x + uintptr_t(ranges[i].bytes))
+                return KVC_ERR_OVERLAP;
+        }
+    const kvc::TableArgs t = {block_tables, context_lens, new_lens, held_blocks, free_blocks, update->q_start, update->context_lens,
+                              update->held_blocks, update->taken, update->slot_map, update->positions, update->row_seqs, desc->num_seqs,
+                              num_free, update->max_rows, desc->max_blocks_per_seq, ilog2(desc->block_size)};
+    const hipError_t e = kvc::launch_block_tables_extend(t, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? KVC_OK : hip_failed(e);
+}
+
+int kvc_kv_cache_write(const void *k_new, const void *v_new, int64_t k_row_stride, int64_t v_row_stride, void *k_cache, void *v_cache,
+                       const int64_t *slot_map, int32_t num_rows, const kvc_attn_desc *desc, void *hip_stream) {
+    const int rc = check_desc(desc);
+    if (rc != KVC_OK) return rc;
+    const int element = desc->dtype == KVC_F32 ? 4 : 2;
+    const int64_t row = int64_t(desc->num_kv_heads) * desc->head_dim, per_word = 16 / element;
+    if (k_row_stride == 0) k_row_stride = row;
+    if (v_row_stride == 0) v_row_stride = row;
+    if (num_rows < 0 || k_row_stride < row || v_row_stride < row) return KVC_ERR_BAD_SHAPE;
+    if (num_rows == 0) return KVC_OK;
+    if (!k_new || !v_new || !k_cache || !v_cache || !slot_map) return KVC_ERR_NULL;
+    if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) || !aligned16(v_cache) || k_row_stride % per_word != 0 ||
+        v_row_stride % per_word != 0)
+        return KVC_ERR_ALIGN;
+    const hipError_t e = kvc::launch_cache_write(k_new, v_new, k_row_stride / per_word, v_row_stride / per_word, k_cache, v_cache, slot_map, num_rows,
+                                                 desc->num_kv_heads, desc->head_dim * element, ilog2(desc->block_size),
+                                                 int64_t(desc->num_pool_blocks) * desc->block_size, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? KVC_OK : hip_failed(e);
+}
+
+int kvc_key_bounds_update(const void *k_cache, void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
+                          const kvc_attn_desc *desc, int32_t max_query_len, void *hip_stream) {
+    const int rc = check_desc(desc);
+    if (rc != KVC_OK) return rc;
+    if (max_query_len < 0 || (!q_start && max_query_len > 1)) return KVC_ERR_BAD_SHAPE;
+    if (desc->num_seqs == 0 || max_query_len == 0) return KVC_OK;
+    if (!k_cache || !bounds || !block_tables || !context_lens) return KVC_ERR_NULL;
+    if (!aligned16(k_cache) || !aligned16(bounds)) return KVC_ERR_ALIGN;
+    const hipError_t e = kvc::launch_key_bounds(k_cache, bounds, block_tables, context_lens, q_start, *desc, ilog2(desc->block_size), max_query_len,
+                                                static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? KVC_OK : hip_failed(e);
+}
+
+size_t kvc_block_select_workspace_bytes(const kvc_attn_desc *desc, int32_t total_q, int32_t budget, int32_t keep_first, int32_t keep_last) {
+    kvc::SelectArgs a;
+    if (select_args(desc, total_q, budget, keep_first, keep_last, &a) != KVC_OK) return 0;
+    return select_bytes(a, total_q);
+}
+
+int kvc_block_select(const void *q, const void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
+                     int32_t *selected, int32_t budget, int32_t keep_first, int32_t keep_last, const kvc_attn_desc *desc, int32_t total_q,
+                     void *workspace, size_t workspace_bytes, void *hip_stream) {
+    kvc::SelectArgs a;
+    const int rc = select_args(desc, total_q, budget, keep_first, keep_last, &a);
+    if (rc != KVC_OK) return rc;
+    if (!q_start && total_q != desc->num_seqs) return KVC_ERR_BAD_SHAPE;
+    if (desc->num_seqs == 0 || total_q == 0) return KVC_OK;
+    if (!q || !bounds || !block_tables || !context_lens || !selected) return KVC_ERR_NULL;
+    if (!aligned16(q) || !aligned16(bounds)) return KVC_ERR_ALIGN;
+    const size_t need = select_bytes(a, total_q);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return KVC_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return KVC_ERR_ALIGN;
+    const hipError_t e = kvc::launch_block_select(q, bounds, block_tables, context_lens, q_start, selected, static_cast<uint64_t *>(workspace), a, total_q,
+                                                  desc->dtype, desc->head_dim, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? KVC_OK : hip_failed(e);
+}
+
+size_t kvc_paged_attention_selected_workspace_bytes(const kvc_attn_desc *desc, int32_t total_q, int32_t budget) {
+    (void)desc;
+    (void)total_q;
+    (void)budget;
+    return 0;
+}
+
+int kvc_paged_attention_selected(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables, const int32_t *context_lens,
+                                 const int32_t *q_start, const int32_t *selected, int32_t budget, float scale, void *out,
+                                 const kvc_attn_desc *desc, int32_t total_q, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    const int rc = check_rows(desc, total_q);
+    if (rc != KVC_OK) return rc;
+    if (budget <= 0 || int64_t(budget) * desc->block_size > 0x40000000 || (!q_start && total_q != desc->num_seqs)) return KVC_ERR_BAD_SHAPE;
+    if (desc->num_seqs == 0 || total_q == 0) return KVC_OK;
+    if (!selected) return KVC_ERR_NULL;
+    const int rc2 = check_attn_args(q, k_cache, v_cache, block_tables, context_lens, scale, out);
+    if (rc2 != KVC_OK) return rc2;
+    (void)workspace;
+    (void)workspace_bytes;
+    kvc::SelectedArgs a = {desc->num_seqs, desc->num_q_heads, desc->num_kv_heads, desc->num_q_heads / desc->num_kv_heads, ilog2(desc->block_size),
+                           desc->max_blocks_per_seq, bound_of(*desc), budget, scale, float(double(scale) * 1.4426950408889634), 0, 0, 0};
+    // units are indexed in 32 bits
+    const bool on_mfma = desc->dtype == KVC_BF16 && desc->block_size >= 4 &&
+                         int64_t(desc->num_pool_blocks) * desc->num_kv_heads * std::max(1, desc->block_size / 16) < (int64_t(1) << 31);
+    const hipError_t e = kvc::launch_attention_selected(q, k_cache, v_cache, block_tables, context_lens, q_start, selected, out, a, total_q, desc->dtype,
+                                                        desc->head_dim, on_mfma, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? KVC_OK : hip_failed(e);
 }
 
 }  // extern "C"

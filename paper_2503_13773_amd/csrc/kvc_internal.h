@@ -125,6 +125,38 @@ constexpr int64_t kCopySlabBytes = 1024;  // bytes one workgroup of the block-co
 hipError_t launch_block_copy(const kvc_pool &src, const kvc_pool &dst, const int64_t *mapping,
                              int64_t num_pairs, hipStream_t stream);
 
+// ---- operators around the cache's blocks
+struct TableArgs {  // kvc_block_tables_extend; held_blocks, held_blocks_out, taken, positions and row_seqs may be null
+    int32_t *block_tables;
+    const int32_t *context_lens, *new_lens, *held_blocks, *free_blocks;
+    int32_t *q_start, *context_lens_out, *held_blocks_out, *taken;
+    int64_t *slot_map;
+    int32_t *positions, *row_seqs;
+    int num_seqs, num_free, max_rows, max_blocks_per_seq, block_size_log2;
+};
+hipError_t launch_block_tables_extend(const TableArgs &t, hipStream_t stream);
+// k_row_words / v_row_words: 16-byte words from one row of k_new / v_new to the next.
+hipError_t launch_cache_write(const void *k_new, const void *v_new, int64_t k_row_words, int64_t v_row_words, void *k_cache, void *v_cache,
+                              const int64_t *slot_map, int num_rows, int num_kv_heads, int row_bytes, int block_size_log2,
+                              int64_t num_slots, hipStream_t stream);
+hipError_t launch_key_bounds(const void *k_cache, void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
+                             const kvc_attn_desc &d, int block_size_log2, int max_query_len, hipStream_t stream);
+struct SelectArgs {
+    int num_seqs, num_q_heads, num_kv_heads, group, block_size_log2, max_blocks_per_seq, max_context_len;
+    int max_blocks;  // keys a (row, KV head) has room for: blocks of max_context_len
+    int budget, keep_first, keep_last;
+};
+hipError_t launch_block_select(const void *q, const void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
+                               int32_t *selected, uint64_t *keys, const SelectArgs &a, int total_q, int dtype, int head_dim, hipStream_t stream);
+struct SelectedArgs {
+    int num_seqs, num_q_heads, num_kv_heads, group, block_size_log2, max_blocks_per_seq, max_context_len, budget;
+    float scale, scale_log2e;
+    int heads_per_chunk, unit_log2, units_per_block_log2;  // set by the launcher
+};
+hipError_t launch_attention_selected(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables, const int32_t *context_lens,
+                                     const int32_t *q_start, const int32_t *selected, void *out, SelectedArgs a, int total_q, int dtype,
+                                     int head_dim, bool on_mfma, hipStream_t stream);
+
 // Largest head chunk (8, 4, 2 or 1) the VALU kernel processes per workgroup for a group size.
 inline int valu_head_chunk(int group) {
     return group % 8 == 0 ? 8 : group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
