@@ -125,6 +125,9 @@ def _calls():
             "kvc_paged_attention_decode", "kvc_paged_attention_decode_workspace_bytes",
             "kvc_paged_attention_decode_scheduled", "kvc_attn_schedule_build", "kvc_paged_attention_prefill",
             "kvc_kv_cache_append", "kvc_kv_block_copy")), AttnDesc)
+        kvc_call.bind_blocks(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
+            "kvc_block_tables_extend", "kvc_kv_cache_write", "kvc_key_bounds_update", "kvc_block_select_workspace_bytes",
+            "kvc_block_select", "kvc_paged_attention_selected_workspace_bytes", "kvc_paged_attention_selected")))
         _native = kvc_call
     return _native
 
@@ -490,6 +493,12 @@ class TableUpdate(NamedTuple):
     row_seqs: torch.Tensor
 
 
+def _here(stream):
+    """(current device, handle of `stream` or of its current stream) for the native calls."""
+    device = torch._C._cuda_getDevice()
+    return device, torch._C._cuda_getCurrentRawStream(device) if stream is None else int(stream.cuda_stream)
+
+
 def _on_stream(stream):
     """Allocations of a call belong to the stream that it works on."""
     return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
@@ -527,6 +536,11 @@ def block_tables_extend(block_tables, context_lens, new_lens, free_blocks, block
                         held_blocks=None, out: Optional[TableUpdate] = None, stream=None) -> TableUpdate:
     """Blocks from the front of free_blocks for new_lens[n] more tokens of every sequence (written into block_tables), and the
     slot, position and sequence of every new token.  A sequence gets all it asks for or nothing (see include/kvc.h)."""
+    if out is not None and max_rows is None and _on_device(block_tables):
+        rc = _calls().extend(block_tables, context_lens, new_lens, held_blocks, free_blocks, block_size, out, *_here(stream))
+        if rc is not None:
+            _check(rc, "kvc_block_tables_extend")
+            return out
     if out is None and max_rows is None:
         raise ValueError("max_rows or out is required")
     if out is None:
@@ -566,6 +580,11 @@ def _row_stride(t) -> int:
 def kv_cache_write(k_new, v_new, k_cache, v_cache, slot_map, stream=None) -> None:
     """Rows k_new[i], v_new[i] ([rows][num_kv_heads][head_dim]; rows may lie apart, as views into a fused projection do) to slot
     slot_map[i] = block * block_size + slot of the caches; a slot outside the pool skips the row."""
+    if _on_device(k_new):
+        rc = _calls().write(k_new, v_new, k_cache, v_cache, slot_map, *_here(stream))
+        if rc is not None:
+            _check(rc, "kvc_kv_cache_write")
+            return
     _require_together(k_cache, v_cache, slot_map)
     ks, vs = _row_stride(k_new), _row_stride(v_new)
     if not (k_new.is_cuda and v_new.is_cuda and k_new.device == v_new.device == k_cache.device):
@@ -598,6 +617,11 @@ def _check_batch(block_tables, context_lens, q_start) -> None:
 def key_bounds_update(k_cache, bounds, block_tables, context_lens, q_start=None, max_query_len: int = 1, stream=None) -> None:
     """Smallest and largest key per channel of every block that the new tokens filled: the last q_start[n+1] - q_start[n] of the
     context_lens[n] tokens of sequence n, or the last one without q_start."""
+    if _on_device(k_cache):
+        rc = _calls().bounds(k_cache, bounds, block_tables, context_lens, q_start, max_query_len, *_here(stream))
+        if rc is not None:
+            _check(rc, "kvc_key_bounds_update")
+            return
     _require_together(k_cache, bounds, block_tables, context_lens, q_start)
     _check_batch(block_tables, context_lens, q_start)
     if k_cache.dim() != 4 or bounds.dtype != k_cache.dtype:
@@ -650,6 +674,12 @@ def block_select(q, bounds, block_tables, context_lens, budget: int, *, block_si
     """The blocks that each query keeps, per KV head: int32 [rows][num_kv_heads][budget], places in the row's block table in
     ascending order, -1 behind them.  The first keep_first and the last keep_last blocks always, the others by the largest
     product that a key inside the block's bounds can have with the query."""
+    if out is not None and _on_device(q):
+        rc = _calls().select(q, bounds, block_tables, context_lens, q_start, budget, block_size, keep_first, keep_last, max_context_len,
+                             out, workspace, *_here(stream))
+        if rc is not None:
+            _check(rc, "kvc_block_select")
+            return out
     desc = _select_desc(q, bounds, block_tables, block_size, max_context_len)
     _check_batch(block_tables, context_lens, q_start)
     shape = (q.shape[0], bounds.shape[1], int(budget))
@@ -685,6 +715,12 @@ def new_selected_workspace(q, k_cache, block_tables, budget: int, *, max_context
 def paged_attention_selected(q, k_cache, v_cache, block_tables, context_lens, selected, scale: float, *, q_start=None, out=None,
                              max_context_len: int = 0, workspace=None, stream=None):
     """out[i,h] = softmax(scale * q[i,h] . K) V over the tokens up to row i's position in the blocks selected[i, h's KV head]."""
+    if out is not None and _on_device(q):
+        rc = _calls().selected(q, k_cache, v_cache, block_tables, context_lens, q_start, selected, scale, out, max_context_len, workspace,
+                               *_here(stream))
+        if rc is not None:
+            _check(rc, "kvc_paged_attention_selected")
+            return out
     desc = _selected_desc(q, k_cache, block_tables, max_context_len)
     _check_batch(block_tables, context_lens, q_start)
     if v_cache.shape != k_cache.shape or v_cache.dtype != q.dtype:
