@@ -431,8 +431,10 @@ KVC_API int kvc_block_select(const void *q, const void *bounds, const int32_t *b
  * Rows, positions and q_start as in kvc_block_select.  A list may be in any order; entries below 0 or past the row's own block are
  * passed over; an entry that appears twice counts twice.  A row whose list leaves nothing gets zeros; rows that belong to no
  * sequence are left as they were.  Accumulation is fp32, output rounded to nearest even.
- *   - workspace: device memory, 256-byte aligned, kvc_paged_attention_selected_workspace_bytes(desc, total_q, budget) of it
- *     (may be NULL when that is 0): scratch, needs no preparation.  Calls that share one must not overlap in time.
+ *   - workspace: device memory, 256-byte aligned, kvc_paged_attention_selected_workspace_bytes(desc, total_q, budget) of it (may be
+ *     NULL when that is 0), with the counter header and the rules of kvc_paged_attention_decode's workspace: prepared once by
+ *     kvc_paged_attention_decode_workspace_init, and one workspace that is large enough may serve both.  Calls that share one must
+ *     not overlap in time.
  */
 KVC_API size_t kvc_paged_attention_selected_workspace_bytes(const kvc_attn_desc *desc, int32_t total_q, int32_t budget);
 KVC_API int kvc_paged_attention_selected(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables,

@@ -649,11 +649,15 @@ def _select_desc(q, bounds, block_tables, block_size, max_context_len) -> AttnDe
     return _rows_desc(q, bounds.shape[0], bounds.shape[1], block_size, block_tables, max_context_len)
 
 
-def _workspace_of(need: int, device, stream=None):
+def _workspace_of(need: int, device, stream=None, counters: bool = False):
+    """Device memory for a call on `stream`; counters: with the header of arrival counters, zeroed."""
     if not need:
         return None
     with _on_stream(stream):
-        return torch.empty(need, dtype=torch.uint8, device=device)
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        if counters:
+            workspace_init(ws)
+        return ws
 
 
 def _workspace_arg(workspace):
@@ -709,7 +713,7 @@ def new_selected_workspace(q, k_cache, block_tables, budget: int, *, max_context
     """A workspace for paged_attention_selected of these shapes (None when it needs none)."""
     desc = _selected_desc(q, k_cache, block_tables, max_context_len)
     return _workspace_of(int(lib().kvc_paged_attention_selected_workspace_bytes(ctypes.byref(desc), q.shape[0], int(budget))),
-                         q.device)
+                         q.device, counters=True)
 
 
 def paged_attention_selected(q, k_cache, v_cache, block_tables, context_lens, selected, scale: float, *, q_start=None, out=None,
@@ -736,7 +740,7 @@ def paged_attention_selected(q, k_cache, v_cache, block_tables, context_lens, se
     budget = selected.shape[2]
     if workspace is None:
         workspace = _workspace_of(int(lib().kvc_paged_attention_selected_workspace_bytes(ctypes.byref(desc), q.shape[0], budget)),
-                                  q.device, stream)
+                                  q.device, stream, counters=True)
     ws, ws_bytes = _workspace_arg(workspace)
     _check(lib().kvc_paged_attention_selected(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(), _ptr(q_start),

@@ -257,6 +257,60 @@ size_t select_bytes(const kvc::SelectArgs &a, int32_t total_q) {
     return size_t(total_q) * a.num_kv_heads * a.max_blocks * sizeof(uint64_t);
 }
 
+// How attention over chosen blocks is cut.  All lists are equally long as far as the host knows.
+struct SelectedPlan {
+    kvc::SelectedArgs a;
+    uint64_t ml_offset, bytes;  // of the workspace: counters, then the parts' accumulators, then their maxima and sums
+};
+constexpr int kSelectedGroups = 512;  // workgroups that few units are cut into
+constexpr int kSelectedManyUnits = 2048;  // from here on a wavefront takes a unit
+int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, SelectedPlan *pl) {
+    const int rc = check_rows(d, total_q);
+    if (rc != KVC_OK) return rc;
+    if (budget <= 0 || int64_t(budget) * d->block_size > 0x40000000) return KVC_ERR_BAD_SHAPE;
+    kvc::SelectedArgs &a = pl->a;
+    a = {};
+    a.num_seqs = d->num_seqs;
+    a.num_q_heads = d->num_q_heads;
+    a.num_kv_heads = d->num_kv_heads;
+    a.group = d->num_q_heads / d->num_kv_heads;
+    a.block_size_log2 = ilog2(d->block_size);
+    a.max_blocks_per_seq = d->max_blocks_per_seq;
+    a.max_context_len = bound_of(*d);
+    a.budget = budget;
+    a.total_q = total_q;
+    // units of a tile are indexed in 32 bits
+    a.on_mfma = d->dtype == KVC_BF16 && d->block_size >= 4 &&
+                int64_t(d->num_pool_blocks) * d->num_kv_heads * std::max(1, d->block_size / 16) < (int64_t(1) << 31);
+    int tiles_of_a_trip;  // what a workgroup's wavefronts take at once
+    if (a.on_mfma) {
+        const int tile_log2 = d->head_dim == 64 ? 5 : 4;
+        const int chunks = int(ceil_div(a.group, 16));
+        a.heads_per_chunk = int(ceil_div(a.group, chunks));
+        a.unit_log2 = std::min(a.block_size_log2, tile_log2);
+        a.units_per_block_log2 = a.block_size_log2 - a.unit_log2;
+        a.tiles = int(ceil_div(int64_t(budget) << a.block_size_log2, 1 << tile_log2));
+        tiles_of_a_trip = kvc::kWaves;
+    } else {
+        a.heads_per_chunk = std::min(4, kvc::valu_head_chunk(a.group));
+        a.tiles = budget;
+        tiles_of_a_trip = std::max(1, 64 >> a.block_size_log2);
+    }
+    const int64_t heads = a.heads_per_chunk, units = int64_t(total_q) * a.num_kv_heads * ceil_div(a.group, heads);
+    a.wave_per_unit = a.on_mfma && units >= kSelectedManyUnits;
+    const int64_t most = std::min<int64_t>(kvc::kMaxSelectedParts, ceil_div(a.tiles, tiles_of_a_trip));
+    const int64_t parts = units > 0 ? std::max<int64_t>(1, std::min<int64_t>(kSelectedGroups / units, most)) : 1;
+    a.tiles_per_part = int(ceil_div(a.tiles, parts));
+    a.parts = int(ceil_div(a.tiles, a.tiles_per_part));
+    pl->ml_offset = pl->bytes = 0;
+    if (a.parts > 1) {
+        const uint64_t slots = uint64_t(units) * a.parts, slot_heads = a.on_mfma ? 16 : heads;
+        pl->ml_offset = kvc::kWorkspaceHeaderBytes + slots * slot_heads * d->head_dim * sizeof(float);
+        pl->bytes = pl->ml_offset + slots * slot_heads * 2 * sizeof(float);
+    }
+    return KVC_OK;
+}
+
 int make_plan(const kvc_attn_desc *d, Plan *pl) {
     const int rc = check_desc(d);
     if (rc != KVC_OK) return rc;
@@ -938,31 +992,32 @@ int kvc_block_select(const void *q, const void *bounds, const int32_t *block_tab
 }
 
 size_t kvc_paged_attention_selected_workspace_bytes(const kvc_attn_desc *desc, int32_t total_q, int32_t budget) {
-    (void)desc;
-    (void)total_q;
-    (void)budget;
-    return 0;
+    SelectedPlan pl;
+    return make_selected_plan(desc, total_q, budget, &pl) == KVC_OK ? size_t(pl.bytes) : 0;
 }
 
 int kvc_paged_attention_selected(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables, const int32_t *context_lens,
                                  const int32_t *q_start, const int32_t *selected, int32_t budget, float scale, void *out,
                                  const kvc_attn_desc *desc, int32_t total_q, void *workspace, size_t workspace_bytes, void *hip_stream) {
-    const int rc = check_rows(desc, total_q);
+    SelectedPlan pl;
+    int rc = make_selected_plan(desc, total_q, budget, &pl);
     if (rc != KVC_OK) return rc;
-    if (budget <= 0 || int64_t(budget) * desc->block_size > 0x40000000 || (!q_start && total_q != desc->num_seqs)) return KVC_ERR_BAD_SHAPE;
+    if (!q_start && total_q != desc->num_seqs) return KVC_ERR_BAD_SHAPE;
     if (desc->num_seqs == 0 || total_q == 0) return KVC_OK;
     if (!selected) return KVC_ERR_NULL;
-    const int rc2 = check_attn_args(q, k_cache, v_cache, block_tables, context_lens, scale, out);
-    if (rc2 != KVC_OK) return rc2;
-    (void)workspace;
-    (void)workspace_bytes;
-    kvc::SelectedArgs a = {desc->num_seqs, desc->num_q_heads, desc->num_kv_heads, desc->num_q_heads / desc->num_kv_heads, ilog2(desc->block_size),
-                           desc->max_blocks_per_seq, bound_of(*desc), budget, scale, float(double(scale) * 1.4426950408889634), 0, 0, 0};
-    // units are indexed in 32 bits
-    const bool on_mfma = desc->dtype == KVC_BF16 && desc->block_size >= 4 &&
-                         int64_t(desc->num_pool_blocks) * desc->num_kv_heads * std::max(1, desc->block_size / 16) < (int64_t(1) << 31);
-    const hipError_t e = kvc::launch_attention_selected(q, k_cache, v_cache, block_tables, context_lens, q_start, selected, out, a, total_q, desc->dtype,
-                                                        desc->head_dim, on_mfma, static_cast<hipStream_t>(hip_stream));
+    rc = check_attn_args(q, k_cache, v_cache, block_tables, context_lens, scale, out);
+    if (rc != KVC_OK) return rc;
+    if (pl.bytes > 0 && (!workspace || workspace_bytes < pl.bytes)) return KVC_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return KVC_ERR_ALIGN;
+    kvc::Workspace ws = {nullptr, nullptr, nullptr};
+    if (pl.bytes > 0) {
+        char *base = static_cast<char *>(workspace);
+        ws = {reinterpret_cast<float *>(base + kvc::kWorkspaceHeaderBytes), reinterpret_cast<float *>(base + pl.ml_offset), reinterpret_cast<int32_t *>(base)};
+    }
+    pl.a.scale = scale;
+    pl.a.scale_log2e = float(double(scale) * 1.4426950408889634);
+    const hipError_t e = kvc::launch_attention_selected(q, k_cache, v_cache, block_tables, context_lens, q_start, selected, out, ws, pl.a, desc->dtype,
+                                                        desc->head_dim, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? KVC_OK : hip_failed(e);
 }
 

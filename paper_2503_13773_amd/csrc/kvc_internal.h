@@ -148,14 +148,16 @@ struct SelectArgs {
 };
 hipError_t launch_block_select(const void *q, const void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
                                int32_t *selected, uint64_t *keys, const SelectArgs &a, int total_q, int dtype, int head_dim, hipStream_t stream);
+constexpr int kMaxSelectedParts = 64;  // parts a list is cut into at most
 struct SelectedArgs {
-    int num_seqs, num_q_heads, num_kv_heads, group, block_size_log2, max_blocks_per_seq, max_context_len, budget;
+    int num_seqs, num_q_heads, num_kv_heads, group, block_size_log2, max_blocks_per_seq, max_context_len, budget, total_q;
     float scale, scale_log2e;
-    int heads_per_chunk, unit_log2, units_per_block_log2;  // set by the launcher
+    // how the work is cut: heads of a KV head in a unit, tiles of a list (vector ALUs: entries), parts of a list and tiles of one
+    int on_mfma, wave_per_unit, heads_per_chunk, unit_log2, units_per_block_log2, tiles, parts, tiles_per_part;
 };
 hipError_t launch_attention_selected(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables, const int32_t *context_lens,
-                                     const int32_t *q_start, const int32_t *selected, void *out, SelectedArgs a, int total_q, int dtype,
-                                     int head_dim, bool on_mfma, hipStream_t stream);
+                                     const int32_t *q_start, const int32_t *selected, void *out, Workspace ws, const SelectedArgs &a, int dtype,
+                                     int head_dim, hipStream_t stream);
 
 // Largest head chunk (8, 4, 2 or 1) the VALU kernel processes per workgroup for a group size.
 inline int valu_head_chunk(int group) {

@@ -3,7 +3,12 @@
 //   out[row][h] = sum_t softmax_t(scale * q[row][h].K[t]) * V[t],  t <= position of the row, t in a block of selected[row][h / group]
 //
 // A list names blocks of the row's own sequence by their place in it, in any order; entries below 0 or past the row's own block are
-// passed over.  One workgroup per (row, KV head, chunk of its heads); its wavefronts take the tiles of the list in turn and meet in LDS.
+// passed over.  A unit of work is (row, KV head, chunk of up to 16 of its heads).  How long a list is the host knows, so the launch is cut
+// into equal parts without looking at the lengths:
+//   few units: the list of each is cut over several workgroups; the last one to finish a part joins all of them
+//     (each stores its part by device-scope accesses, waits for the stores and counts itself; nobody waits for anybody);
+//   more: a workgroup per unit, whose wavefronts take the tiles of the list in turn and meet in LDS;
+//   many: a wavefront per unit, nothing to join.
 #include "cache_rows.h"
 #include "kvc_internal.h"
 #include "pa_partials.h"
@@ -14,7 +19,7 @@ namespace {
 
 using namespace mfma;
 
-constexpr int kWindow = 512;  // units whose places are held in LDS at a time
+constexpr int kWindow = 512;  // list entries whose places are held in LDS at a time (vector ALUs)
 
 // ---- bf16 on the matrix cores, up to 16 heads of a KV head (blocks of 4 tokens and more)
 
@@ -26,15 +31,15 @@ __device__ inline void split_weights(float p0, float p1, uint32_t *hi, uint32_t 
                     __builtin_fmaf(p1, 1.f + FLT_EPSILON, -__uint_as_float(u1 & 0xffff0000u)));
 }
 
-// limit[h]: how many of this lane's tokens 16 h + 4 quad .. + 3 of the tile count.
-__device__ inline void attend_tile(HeadStateN<8> &st, Shape<128>::Tile &t, const bf16x8 (&qb)[4], float scale_log2e, const int (&limit)[1]) {
+// limit[h]: how many of this lane's tokens 16 h + 4 quad .. + 3 of the tile count; full: all of every lane's.
+__device__ inline void attend_tile(HeadStateN<8> &st, Shape<128>::Tile &t, const bf16x8 (&qb)[4], float scale_log2e, const int (&limit)[1], bool full) {
     floatx4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[j]), qb[j], s, 0, 0, 0);
     float sv[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) sv[i] = s[i] * scale_log2e;
-    if (__builtin_amdgcn_ballot_w64(limit[0] < 4) != 0) {
+    if (!full) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (i >= limit[0]) {
@@ -70,7 +75,7 @@ __device__ inline void attend_tile(HeadStateN<8> &st, Shape<128>::Tile &t, const
     }
 }
 
-__device__ inline void attend_tile(HeadStateN<4> &st, Shape<64>::Tile &t, const bf16x8 (&qb)[2], float scale_log2e, const int (&limit)[2]) {
+__device__ inline void attend_tile(HeadStateN<4> &st, Shape<64>::Tile &t, const bf16x8 (&qb)[2], float scale_log2e, const int (&limit)[2], bool full) {
     float sv[8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -80,7 +85,7 @@ __device__ inline void attend_tile(HeadStateN<4> &st, Shape<64>::Tile &t, const 
 #pragma unroll
         for (int i = 0; i < 4; ++i) sv[4 * h + i] = s[i] * scale_log2e;
     }
-    if (__builtin_amdgcn_ballot_w64(limit[0] + limit[1] < 8) != 0) {
+    if (!full) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if ((i & 3) >= limit[i >> 2]) {
@@ -139,88 +144,198 @@ struct ListOf {
     }
 };
 
-template <int HD>
-__global__ __launch_bounds__(kThreads, 2) void pa_selected_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache,
-                                                                       const uint16_t *__restrict__ v_cache, const int32_t *__restrict__ block_tables,
-                                                                       const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start,
-                                                                       const int32_t *__restrict__ selected, uint16_t *__restrict__ out, SelectedArgs a) {
+// Tiles first, first + step, ... below `tiles` of a list's part that begins at tile0.  Whether any token counted.  A lane holds the place of
+// one unit; 64 >> units_log2 tiles are known at a time.  UNIFORM: units of 16 tokens and more, whose places are the same for all lanes.
+template <int HD, bool UNIFORM>
+__device__ inline bool attend_list(typename Shape<HD>::State &st, const bf16x8 (&qb)[Shape<HD>::kQ], const uint16_t *__restrict__ k_cache,
+                                   const uint16_t *__restrict__ v_cache, const ListOf &list, float scale_log2e, int tile0, int tiles, int first, int step) {
     using TS = Shape<HD>;
-    constexpr int kTokens = TS::kTokens, kSubs = kTokens / 16, NV = TS::kVecs;
-    __shared__ int2 s_unit[kWindow];
-    __shared__ int s_last;
-    __shared__ float4 s_acc[kWaves][16 * HD / 4];
-    __shared__ float2 s_ml[kWaves][16];
-    const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, quad = lane >> 4, r = lane & 15;
-    const int kvh = blockIdx.x % a.num_kv_heads, row = blockIdx.x / a.num_kv_heads;
-    const int head0 = kvh * a.group + blockIdx.y * a.heads_per_chunk, heads = min(a.heads_per_chunk, (kvh + 1) * a.group - head0);
-    int n, pos;
-    if (!find_row(row, q_start, context_lens, a.num_seqs, a.max_context_len, &n, &pos)) return;
-    uint16_t *dst = out + (int64_t(row) * a.num_q_heads + head0) * HD;
-    auto write_zeros = [&]() {
-        for (int i = tid; i < heads * HD / 8; i += kThreads) reinterpret_cast<uint4 *>(dst)[i] = uint4{0u, 0u, 0u, 0u};
+    using Tile = typename TS::Tile;
+    constexpr int kSubs = TS::kTokens / 16;
+    struct Piece {
+        Tile t;
+        int limit[kSubs];
+        bool full;
     };
-    if (pos < 0) return write_zeros();
-    bf16x8 qb[TS::kQ];
-    load_q_operand(qb, q + (int64_t(row) * a.num_q_heads + head0 + (r < heads ? r : 0)) * HD, quad, r < heads);
-    const int32_t *table = block_tables + int64_t(n) * a.max_blocks_per_seq;
-    const ListOf list = {selected + (int64_t(row) * a.num_kv_heads + kvh) * a.budget, table, pos, table[pos >> a.block_size_log2],
-                         a.num_kv_heads, kvh, a.block_size_log2, a.unit_log2, a.units_per_block_log2, a.budget};
-    const int units_log2 = TS::kTokensLog2 - a.unit_log2, units = a.budget << a.units_per_block_log2;  // of a tile; of the list
-    const int unit_tokens = 1 << a.unit_log2, k_off = (r & (unit_tokens - 1)) * HD + 8 * quad, v_off = ((4 * quad) & (unit_tokens - 1)) * HD + HD / 16 * r;
+    const int lane = threadIdx.x & 63, quad = lane >> 4, r = lane & 15;
+    const int unit_log2 = list.unit_log2, units_log2 = TS::kTokensLog2 - unit_log2, unit_tokens = 1 << unit_log2;
+    const int k_off = (r & (unit_tokens - 1)) * HD + 8 * quad, v_off = ((4 * quad) & (unit_tokens - 1)) * HD + HD / 16 * r;
     const size_t unit_elems = size_t(unit_tokens) * HD;
+    bool any = false;
+    for (int from = first; from < tiles; from += step << (6 - units_log2)) {
+        const int mine = from + step * (lane >> units_log2);
+        int2 e = {0, 0};
+        if (mine < tiles) e = list.unit(((tile0 + mine) << units_log2) + (lane & ((1 << units_log2) - 1)));
+        const uint64_t there = __ballot(e.y > 0);
+        if (there == 0) continue;
+        any = true;
+        const int count = ((63 - __builtin_clzll(there)) >> units_log2) + 1;
+        auto issue = [&](Piece &x, int i) __attribute__((always_inline)) {
+            bool full = true;
+#pragma unroll
+            for (int h = 0; h < kSubs; ++h) {
+                const uint16_t *kp, *vp;
+                if constexpr (UNIFORM) {
+                    // a unit is the tile, or (32-token tiles, blocks of 16) half of it
+                    const bool half = kSubs == 2 && units_log2 == 1;
+                    const int at = half ? 2 * i + h : i, in_unit = half ? 0 : 16 * h;
+                    const size_t base = size_t(uint32_t(__builtin_amdgcn_readlane(e.x, at))) * unit_elems + in_unit * HD;
+                    const int counts = __builtin_amdgcn_readlane(e.y, at) - in_unit;
+                    kp = k_cache + base + k_off;
+                    vp = v_cache + base + v_off;
+                    full &= counts >= 16;
+                    x.limit[h] = min(max(counts - 4 * quad, 0), 4);
+                } else {
+                    const int k_at = (i << units_log2) + ((16 * h + r) >> unit_log2), v_at = (i << units_log2) + ((16 * h + 4 * quad) >> unit_log2);
+                    kp = k_cache + size_t(uint32_t(__shfl(e.x, k_at))) * unit_elems + k_off;
+                    vp = v_cache + size_t(uint32_t(__shfl(e.x, v_at))) * unit_elems + v_off;
+                    x.limit[h] = min(max(__shfl(e.y, v_at) - ((4 * quad) & (unit_tokens - 1)), 0), 4);
+                    full &= __ballot(x.limit[h] < 4) == 0;
+                }
+                if constexpr (HD == 128) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x.t.k[j] = load16_stream(kp + 32 * j);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x.t.v[j] = load16_stream(vp + j * HD);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) x.t.k[2 * h + j] = load16_stream(kp + 32 * j);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x.t.v[4 * h + j] = load8_stream(vp + j * HD);
+                }
+            }
+            x.full = full;
+        };
+        auto compute = [&](Piece &x) __attribute__((always_inline)) { attend_tile(st, x.t, qb, scale_log2e, x.limit, x.full); };
+        Piece A, B;
+        issue(A, 0);
+        int i = 0;
+        for (; i + 2 < count; i += 2) {
+            issue(B, i + 1);
+            compute(A);
+            issue(A, i + 2);
+            compute(B);
+        }
+        if (i + 1 < count) {
+            issue(B, i + 1);
+            compute(A);
+            compute(B);
+        } else {
+            compute(A);
+        }
+    }
+    return any;
+}
+
+// The row, KV head and heads of a unit.
+struct Unit {
+    int row, kvh, head0, heads, n, pos;
+    bool there;  // the row belongs to a sequence
+    __device__ Unit(const SelectedArgs &a, const int32_t *q_start, const int32_t *context_lens, int row_, int kvh_, int chunk) {
+        row = row_;
+        kvh = kvh_;
+        head0 = kvh * a.group + chunk * a.heads_per_chunk;
+        heads = min(a.heads_per_chunk, (kvh + 1) * a.group - head0);
+        there = find_row(row, q_start, context_lens, a.num_seqs, a.max_context_len, &n, &pos);
+    }
+};
+__device__ inline ListOf list_of(const SelectedArgs &a, const Unit &u, const int32_t *selected, const int32_t *block_tables) {
+    const int32_t *table = block_tables + int64_t(u.n) * a.max_blocks_per_seq;
+    return ListOf{selected + (int64_t(u.row) * a.num_kv_heads + u.kvh) * a.budget, table, u.pos, table[u.pos >> a.block_size_log2],
+                  a.num_kv_heads, u.kvh, a.block_size_log2, a.unit_log2, a.units_per_block_log2, a.budget};
+}
+
+// A wavefront per unit; blockIdx.x = KV head + KV heads * group of kWaves rows, so that with 8 KV heads each XCD keeps one.
+template <int HD, bool UNIFORM>
+__global__ __launch_bounds__(kThreads, 3) void pa_selected_wave_kernel(
+    const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache, const uint16_t *__restrict__ v_cache, const int32_t *__restrict__ block_tables,
+    const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start, const int32_t *__restrict__ selected, uint16_t *__restrict__ out,
+    SelectedArgs a) {
+    using TS = Shape<HD>;
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, quad = lane >> 4, r = lane & 15;
+    const int group = blockIdx.x / a.num_kv_heads, row = group * kWaves + wave;
+    if (row >= a.total_q) return;
+    const Unit u(a, q_start, context_lens, row, blockIdx.x - group * a.num_kv_heads, blockIdx.y);
+    if (!u.there) return;
+    uint16_t *dst = out + (int64_t(row) * a.num_q_heads + u.head0 + r) * HD + HD / 4 * quad;
     typename TS::State st;
     st.reset();
     bool any = false;
-    for (int u0 = 0; u0 < units; u0 += kWindow) {
-        if (tid == 0) s_last = 0;
-        __syncthreads();
-        int last = 0;
-        for (int i = tid; i < kWindow; i += kThreads) {
-            const int2 e = list.unit(u0 + i);
-            s_unit[i] = e;
-            if (e.y > 0) last = i + 1;
-        }
-        if (last > 0) atomicMax(&s_last, last);
-        __syncthreads();
-        const int tiles = (s_last + (1 << units_log2) - 1) >> units_log2;
-        any |= tiles > 0;
-        for (int it = wave; it < tiles; it += kWaves) {
-            typename TS::Tile t;
-            int limit[kSubs];
-#pragma unroll
-            for (int h = 0; h < kSubs; ++h) {
-                const int2 *e = s_unit + (it << units_log2);
-                const int kt = 16 * h + r, vt = 16 * h + 4 * quad;  // tokens of the tile
-                const uint16_t *kp = k_cache + size_t(e[kt >> a.unit_log2].x) * unit_elems + k_off;
-                const int2 ve = e[vt >> a.unit_log2];
-                const uint16_t *vp = v_cache + size_t(ve.x) * unit_elems + v_off;
-                limit[h] = min(max(ve.y - (vt & (unit_tokens - 1)), 0), 4);
-                if constexpr (HD == 128) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) t.k[j] = load16_stream(kp + 32 * j);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) t.v[i] = load16_stream(vp + i * HD);
-                } else {
-                    const int in_unit = a.unit_log2 == 5 ? 16 * h * HD : 0;  // second half of a unit of 32 tokens
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) t.k[2 * h + j] = load16_stream(kp + in_unit + 32 * j);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) t.v[4 * h + i] = load8_stream(vp + in_unit + i * HD);
-                }
-            }
-            attend_tile(st, t, qb, a.scale_log2e, limit);
-        }
-        __syncthreads();
+    if (u.pos >= 0) {
+        bf16x8 qb[TS::kQ];
+        load_q_operand(qb, q + (int64_t(row) * a.num_q_heads + u.head0 + (r < u.heads ? r : 0)) * HD, quad, r < u.heads);
+        any = attend_list<HD, UNIFORM>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, 0, a.tiles, 0, 1);
     }
-    if (!any) return write_zeros();
     st.finish();
+    if (r >= u.heads) return;
+    const float inv = 1.0f / st.l;
+#pragma unroll
+    for (int v = 0; v < TS::kVecs; v += 2) {
+        const float4 x = acc_vec(st, v), y = acc_vec(st, v + 1);
+        const uint4 w = {pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv), pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv)};
+        *reinterpret_cast<uint4 *>(dst + 4 * v) = any ? w : uint4{0u, 0u, 0u, 0u};
+    }
+}
+
+// A workgroup per part of a unit's list; blockIdx.x = KV head + KV heads * row, blockIdx.y = chunk of heads, blockIdx.z = part.
+template <int HD, bool UNIFORM>
+__global__ __launch_bounds__(kThreads, 2) void pa_selected_mfma_kernel(
+    const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache, const uint16_t *__restrict__ v_cache, const int32_t *__restrict__ block_tables,
+    const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start, const int32_t *__restrict__ selected, uint16_t *__restrict__ out,
+    Workspace ws, SelectedArgs a) {
+    using TS = Shape<HD>;
+    constexpr int NV = TS::kVecs;
+    __shared__ float4 s_acc[kWaves][16 * HD / 4];
+    __shared__ float2 s_ml[kMaxSelectedParts][16];  // of the wavefronts, then of the parts
+    __shared__ int s_last;
+    const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, quad = lane >> 4, r = lane & 15;
+    const int row = blockIdx.x / a.num_kv_heads, parts = a.parts, part = blockIdx.z;
+    const Unit u(a, q_start, context_lens, row, blockIdx.x - row * a.num_kv_heads, blockIdx.y);
+    if (!u.there) return;
+    uint16_t *dst = out + (int64_t(row) * a.num_q_heads + u.head0) * HD;
+    if (u.pos < 0) {
+        if (part == 0)
+            for (int i = tid; i < u.heads * HD / 8; i += kThreads) reinterpret_cast<uint4 *>(dst)[i] = uint4{0u, 0u, 0u, 0u};
+        return;
+    }
+    bf16x8 qb[TS::kQ];
+    load_q_operand(qb, q + (int64_t(row) * a.num_q_heads + u.head0 + (r < u.heads ? r : 0)) * HD, quad, r < u.heads);
+    typename TS::State st;
+    st.reset();
+    const int tile0 = part * a.tiles_per_part;
+    const bool any = attend_list<HD, UNIFORM>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, tile0,
+                                              min(a.tiles_per_part, a.tiles - tile0), wave, kWaves);
+    st.finish();
+    // a wavefront or part without a token says so with a maximum of -inf (with tokens it is -FLT_MAX at least)
 #pragma unroll
     for (int v = 0; v < NV; ++v) s_acc[wave][(v * 4 + quad) * 16 + r] = acc_vec(st, v);
-    if (quad == 0) s_ml[wave][r] = float2{st.m, st.l};
+    if (quad == 0) s_ml[wave][r] = float2{any ? st.m : -INFINITY, st.l};
     __syncthreads();
-    for (int f = tid; f < heads * HD / 4; f += kThreads) {
-        const int head = f / (HD / 4), d = f % (HD / 4);  // dims 4 d .. 4 d + 3
-        const int vq = (d % NV) * 4 + d / NV;             // a quad holds HD / 4 dims, NV vectors
+    const int vecs = u.heads * HD / 4;
+    const int64_t slot0 = (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * parts;
+    const uint32_t slots = uint32_t(gridDim.x * gridDim.y) * parts, slot_vecs = 16 * HD / 4;
+    const __amdgpu_buffer_rsrc_t acc_buf = raw_buffer(ws.acc, parts > 1 ? slots * slot_vecs * 16u : 0u), ml_buf = raw_buffer(ws.ml, parts > 1 ? slots * 16u * 8u : 0u);
+    // vector f of the output: dims 4 d .. 4 d + 3 of a head
+    auto place = [&](int f, int *head) __attribute__((always_inline)) {
+        *head = f / (HD / 4);
+        const int d = f % (HD / 4);
+        return ((d % NV) * 4 + d / NV) * 16 + *head;  // a quad holds HD / 4 dims, NV vectors
+    };
+    auto add = [](float4 &x, float w, const float4 &y) __attribute__((always_inline)) {
+        x.x = fmaf(w, y.x, x.x);
+        x.y = fmaf(w, y.y, x.y);
+        x.z = fmaf(w, y.z, x.z);
+        x.w = fmaf(w, y.w, x.w);
+    };
+    auto write_out = [&](int f, const float4 &x, float M, float L) __attribute__((always_inline)) {
+        const float inv = 1.0f / L;  // no token in the list: zeros
+        const uint2 w = {pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv)};
+        reinterpret_cast<uint2 *>(dst)[f] = M == -INFINITY ? uint2{0u, 0u} : w;
+    };
+    auto weight = [](float m, float M) __attribute__((always_inline)) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M); };
+    for (int f = tid; f < vecs; f += kThreads) {
+        int head;
+        const int at = place(f, &head);
         float M = -INFINITY, L = 0.f;
         float4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -228,16 +343,54 @@ __global__ __launch_bounds__(kThreads, 2) void pa_selected_mfma_kernel(const uin
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const float2 ml = s_ml[w][head];
-            const float wgt = __builtin_amdgcn_exp2f(ml.x - M);
-            const float4 y = s_acc[w][vq * 16 + head];
+            const float wgt = weight(ml.x, M);
             L = fmaf(wgt, ml.y, L);
-            x.x = fmaf(wgt, y.x, x.x);
-            x.y = fmaf(wgt, y.y, x.y);
-            x.z = fmaf(wgt, y.z, x.z);
-            x.w = fmaf(wgt, y.w, x.w);
+            add(x, wgt, s_acc[w][at]);
         }
-        const float inv = 1.0f / L;
-        reinterpret_cast<uint2 *>(dst)[f] = uint2{pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv)};
+        if (parts == 1) {
+            write_out(f, x, M, L);
+        } else {
+            store4_device_scope(acc_buf, (uint32_t(slot0 + part) * slot_vecs + at) * 16u, x.x, x.y, x.z, x.w);
+            if (f % (HD / 4) == 0) store2_device_scope(ml_buf, (uint32_t(slot0 + part) * 16u + head) * 8u, M, L);
+        }
+    }
+    if (parts == 1) return;
+    // the count may become visible only after the part: every wavefront waits for its own stores, then all meet
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    int32_t *const counter = ws.cnt + blockIdx.x * gridDim.y + blockIdx.y;
+    if (tid == 0) s_last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");  // the fetches stay behind the count
+    if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int i = tid; i < parts * u.heads; i += kThreads) {
+        const int p = i / u.heads, head = i - p * u.heads;
+        s_ml[p][head] = load2_device_scope(ml_buf, (uint32_t(slot0 + p) * 16u + head) * 8u);
+    }
+    __syncthreads();
+    for (int f = tid; f < vecs; f += kThreads) {
+        int head;
+        const int at = place(f, &head);
+        float M = -INFINITY, L = 0.f;
+        float4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < parts; ++p) M = fmaxf(M, s_ml[p][head].x);
+        constexpr int kBatch = 8;
+        for (int p0 = 0; p0 < parts; p0 += kBatch) {
+            float4 y[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) y[j] = load4_device_scope(acc_buf, (uint32_t(slot0 + min(p0 + j, parts - 1)) * slot_vecs + at) * 16u);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if (p0 + j >= parts) break;
+                const float2 ml = s_ml[p0 + j][head];
+                const float wgt = weight(ml.x, M);
+                L = fmaf(wgt, ml.y, L);
+                add(x, wgt, y[j]);
+            }
+        }
+        write_out(f, x, M, L);
     }
 }
 
@@ -270,44 +423,63 @@ struct Vec<uint16_t> {
     __device__ static uint16_t out(float x) { return f32_to_bf16_rne(x); }
 };
 
+// x summed over aligned groups of LR lanes (8, 16 or 32) inside the vector ALU.
+template <int LR>
+__device__ inline float sum_over_lanes(float x) {
+    x += lanes::permuted<lanes::kXor1>(x);
+    x += lanes::permuted<lanes::kXor2>(x);
+    x += lanes::permuted<lanes::kMirror8>(x);
+    if constexpr (LR > 8) x += lanes::permuted<lanes::kMirror16>(x);
+    if constexpr (LR > 16) {
+        const lanes::Pair<float> b = lanes::pair_of<16>(x);
+        x = b.first + b.second;
+    }
+    return x;
+}
+__device__ inline void store_device(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline float load_device(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Grid as above, the chunk of heads HEADS of them.
 template <class T, int D, int HEADS>
 __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__restrict__ q, const T *__restrict__ k_cache, const T *__restrict__ v_cache,
                                                                     const int32_t *__restrict__ block_tables, const int32_t *__restrict__ context_lens,
                                                                     const int32_t *__restrict__ q_start, const int32_t *__restrict__ selected,
-                                                                    T *__restrict__ out, SelectedArgs a) {
+                                                                    T *__restrict__ out, Workspace ws, SelectedArgs a) {
     constexpr int N = Vec<T>::N, LR = D / N, TOKENS = 64 / LR, U = 4;
     __shared__ int2 s_entry[kWindow];  // pool index of a block, tokens of it that count
     __shared__ int s_last;
-    __shared__ float s_m[kWaves][HEADS], s_l[kWaves][HEADS], s_acc[kWaves][HEADS][D];
+    __shared__ float s_m[kMaxSelectedParts][HEADS], s_l[kMaxSelectedParts][HEADS], s_acc[kWaves][HEADS][D];  // of the wavefronts; m, l of the parts
     const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, c = lane % LR, tg = lane / LR;
-    const int kvh = blockIdx.x % a.num_kv_heads, row = blockIdx.x / a.num_kv_heads, head0 = kvh * a.group + blockIdx.y * HEADS;
-    int n, pos;
-    if (!find_row(row, q_start, context_lens, a.num_seqs, a.max_context_len, &n, &pos)) return;
-    T *dst = out + (int64_t(row) * a.num_q_heads + head0) * D;
-    if (pos < 0) {
-        for (int i = tid; i < HEADS * D; i += kThreads) dst[i] = T(0);
+    const int row = blockIdx.x / a.num_kv_heads, parts = a.parts, part = blockIdx.z;
+    const Unit u(a, q_start, context_lens, row, blockIdx.x - row * a.num_kv_heads, blockIdx.y);
+    if (!u.there) return;
+    T *dst = out + (int64_t(row) * a.num_q_heads + u.head0) * D;
+    if (u.pos < 0) {
+        if (part == 0)
+            for (int i = tid; i < HEADS * D; i += kThreads) dst[i] = T(0);
         return;
     }
     float x[HEADS][N], m[HEADS], l[HEADS], acc[HEADS][N];
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {
-        Vec<T>::get(*reinterpret_cast<const uint4 *>(q + (int64_t(row) * a.num_q_heads + head0 + h) * D + c * N), x[h]);
+        Vec<T>::get(*reinterpret_cast<const uint4 *>(q + (int64_t(row) * a.num_q_heads + u.head0 + h) * D + c * N), x[h]);
         m[h] = -FLT_MAX;
         l[h] = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) acc[h][i] = 0.f;
     }
-    const int32_t *list = selected + (int64_t(row) * a.num_kv_heads + kvh) * a.budget, *table = block_tables + int64_t(n) * a.max_blocks_per_seq;
-    const int bs_log2 = a.block_size_log2, own = pos >> bs_log2, own_block = table[own];
+    const int32_t *list = selected + (int64_t(row) * a.num_kv_heads + u.kvh) * a.budget, *table = block_tables + int64_t(u.n) * a.max_blocks_per_seq;
+    const int bs_log2 = a.block_size_log2, own = u.pos >> bs_log2, own_block = table[own];
+    const int end = min(a.budget, (part + 1) * a.tiles_per_part);  // here a tile is a list entry
     bool any = false;
-    for (int e0 = 0; e0 < a.budget; e0 += kWindow) {
+    for (int e0 = part * a.tiles_per_part; e0 < end; e0 += kWindow) {
         if (tid == 0) s_last = 0;
         __syncthreads();
         int last = 0;
-        for (int i = tid; i < min(kWindow, a.budget - e0); i += kThreads) {
+        for (int i = tid; i < min(kWindow, end - e0); i += kThreads) {
             const int b = list[e0 + i];
             const bool there = b >= 0 && b <= own;
-            s_entry[i] = int2{there ? table[b] : own_block, there ? min(pos + 1 - (b << bs_log2), 1 << bs_log2) : 0};
+            s_entry[i] = int2{there ? table[b] : own_block, there ? min(u.pos + 1 - (b << bs_log2), 1 << bs_log2) : 0};
             if (there) last = i + 1;
         }
         if (last > 0) atomicMax(&s_last, last);
@@ -318,41 +490,41 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
             float kf[U][N], vf[U][N];
             bool counts[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int t = t0 + u * TOKENS + tg;
+            for (int i = 0; i < U; ++i) {
+                const int t = t0 + i * TOKENS + tg;
                 const int2 e = s_entry[min(t, tokens - 1) >> bs_log2];
                 const int slot = t & ((1 << bs_log2) - 1);
-                counts[u] = t < tokens && slot < e.y;
-                const int64_t at = (((int64_t(e.x) * a.num_kv_heads + kvh) << bs_log2) + (counts[u] ? slot : 0)) * D + c * N;
-                Vec<T>::get(*reinterpret_cast<const uint4 *>(k_cache + at), kf[u]);
-                Vec<T>::get(*reinterpret_cast<const uint4 *>(v_cache + at), vf[u]);
-#pragma unroll
-                for (int i = 0; i < N; ++i) vf[u][i] = counts[u] ? vf[u][i] : 0.f;
+                counts[i] = t < tokens && slot < e.y;
+                const int64_t at = (((int64_t(e.x) * a.num_kv_heads + u.kvh) << bs_log2) + (counts[i] ? slot : 0)) * D + c * N;
+                Vec<T>::get(*reinterpret_cast<const uint4 *>(k_cache + at), kf[i]);
+                Vec<T>::get(*reinterpret_cast<const uint4 *>(v_cache + at), vf[i]);
             }
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) vf[i][j] = counts[i] ? vf[i][j] : 0.f;
 #pragma unroll
             for (int h = 0; h < HEADS; ++h) {
                 float s[U], top = m[h];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
+                for (int i = 0; i < U; ++i) {
                     float d = 0.f;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) d = fmaf(x[h][i], kf[u][i], d);
-#pragma unroll
-                    for (int off = 1; off < LR; off <<= 1) d += __shfl_xor(d, off);
-                    s[u] = counts[u] ? d * a.scale : -INFINITY;
-                    top = fmaxf(top, s[u]);
+                    for (int j = 0; j < N; ++j) d = fmaf(x[h][j], kf[i][j], d);
+                    s[i] = counts[i] ? sum_over_lanes<LR>(d) * a.scale : -INFINITY;
+                    top = fmaxf(top, s[i]);
                 }
                 const float alpha = expf(m[h] - top);
                 m[h] = top;
                 l[h] *= alpha;
 #pragma unroll
-                for (int i = 0; i < N; ++i) acc[h][i] *= alpha;
+                for (int j = 0; j < N; ++j) acc[h][j] *= alpha;
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const float p = expf(s[u] - top);
+                for (int i = 0; i < U; ++i) {
+                    const float p = expf(s[i] - top);
                     l[h] += p;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) acc[h][i] = fmaf(p, vf[u][i], acc[h][i]);
+                    for (int j = 0; j < N; ++j) acc[h][j] = fmaf(p, vf[i][j], acc[h][j]);
                 }
             }
         }
@@ -378,6 +550,7 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
         }
     }
     __syncthreads();
+    const int64_t unit = int64_t(blockIdx.x) * gridDim.y + blockIdx.y, slot0 = unit * parts;
     for (int f = tid; f < HEADS * D; f += kThreads) {
         const int h = f / D, d = f % D;
         float M = -FLT_MAX, L = 0.f, A = 0.f;
@@ -387,41 +560,84 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
             L = fmaf(wgt, s_l[w][h], L);
             A = fmaf(wgt, s_acc[w][h][d], A);
         }
-        dst[f] = Vec<T>::out(any ? A / L : 0.f);
+        if (parts == 1) {
+            dst[f] = Vec<T>::out(any ? A / L : 0.f);
+        } else {
+            store_device(ws.acc + (slot0 + part) * (HEADS * D) + f, A);
+            if (d == 0) {  // a part without a token says so
+                store_device(ws.ml + ((slot0 + part) * HEADS + h) * 2, any ? M : -INFINITY);
+                store_device(ws.ml + ((slot0 + part) * HEADS + h) * 2 + 1, L);
+            }
+        }
+    }
+    if (parts == 1) return;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");  // as above
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) s_last = __hip_atomic_fetch_add(ws.cnt + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    if (tid == 0) __hip_atomic_store(ws.cnt + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int i = tid; i < parts * HEADS; i += kThreads) {
+        s_m[i / HEADS][i % HEADS] = load_device(ws.ml + (slot0 * HEADS + i) * 2);
+        s_l[i / HEADS][i % HEADS] = load_device(ws.ml + (slot0 * HEADS + i) * 2 + 1);
+    }
+    __syncthreads();
+    for (int f = tid; f < HEADS * D; f += kThreads) {
+        const int h = f / D;
+        float M = -INFINITY, L = 0.f, A = 0.f;
+        for (int p = 0; p < parts; ++p) M = fmaxf(M, s_m[p][h]);
+        constexpr int kBatch = 8;
+        for (int p0 = 0; p0 < parts; p0 += kBatch) {
+            float y[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) y[j] = load_device(ws.acc + (slot0 + min(p0 + j, parts - 1)) * (HEADS * D) + f);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if (p0 + j >= parts) break;
+                const float wgt = s_m[p0 + j][h] == -INFINITY ? 0.f : expf(s_m[p0 + j][h] - M);
+                L = fmaf(wgt, s_l[p0 + j][h], L);
+                A = fmaf(wgt, y[j], A);
+            }
+        }
+        dst[f] = Vec<T>::out(M == -INFINITY ? 0.f : A / L);
     }
 }
 
 }  // namespace
 
 hipError_t launch_attention_selected(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables, const int32_t *context_lens,
-                                     const int32_t *q_start, const int32_t *selected, void *out, SelectedArgs a, int total_q, int dtype,
-                                     int head_dim, bool on_mfma, hipStream_t stream) {
-    const unsigned pairs = unsigned(int64_t(total_q) * a.num_kv_heads);
-    if (on_mfma) {
-        const int tile_log2 = head_dim == 64 ? 5 : 4;
-        a.unit_log2 = std::min(a.block_size_log2, tile_log2);
-        a.units_per_block_log2 = a.block_size_log2 - a.unit_log2;
-        const int chunks = (a.group + 15) / 16;
-        a.heads_per_chunk = (a.group + chunks - 1) / chunks;
-        auto launch = [&](auto kernel) {
-            kernel<<<dim3(pairs, unsigned((a.group + a.heads_per_chunk - 1) / a.heads_per_chunk)), dim3(kThreads), 0, stream>>>(
-                static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_cache), static_cast<const uint16_t *>(v_cache), block_tables, context_lens,
-                q_start, selected, static_cast<uint16_t *>(out), a);
-        };
-        if (head_dim == 64) launch(pa_selected_mfma_kernel<64>); else launch(pa_selected_mfma_kernel<128>);
+                                     const int32_t *q_start, const int32_t *selected, void *out, Workspace ws, const SelectedArgs &a, int dtype,
+                                     int head_dim, hipStream_t stream) {
+    const unsigned chunks = unsigned((a.group + a.heads_per_chunk - 1) / a.heads_per_chunk);
+    const dim3 grid(unsigned(a.total_q) * unsigned(a.num_kv_heads), chunks, unsigned(a.parts));
+    if (a.on_mfma) {
+        const auto *qp = static_cast<const uint16_t *>(q), *kp = static_cast<const uint16_t *>(k_cache), *vp = static_cast<const uint16_t *>(v_cache);
+        auto *op = static_cast<uint16_t *>(out);
+        const bool uniform = a.unit_log2 >= 4;
+        if (a.wave_per_unit) {
+            const dim3 waves(unsigned((a.total_q + kWaves - 1) / kWaves) * unsigned(a.num_kv_heads), chunks);
+            auto launch = [&](auto kernel) { kernel<<<waves, dim3(kThreads), 0, stream>>>(qp, kp, vp, block_tables, context_lens, q_start, selected, op, a); };
+            if (head_dim == 64) uniform ? launch(pa_selected_wave_kernel<64, true>) : launch(pa_selected_wave_kernel<64, false>);
+            else uniform ? launch(pa_selected_wave_kernel<128, true>) : launch(pa_selected_wave_kernel<128, false>);
+        } else {
+            auto launch = [&](auto kernel) { kernel<<<grid, dim3(kThreads), 0, stream>>>(qp, kp, vp, block_tables, context_lens, q_start, selected, op, ws, a); };
+            if (head_dim == 64) uniform ? launch(pa_selected_mfma_kernel<64, true>) : launch(pa_selected_mfma_kernel<64, false>);
+            else uniform ? launch(pa_selected_mfma_kernel<128, true>) : launch(pa_selected_mfma_kernel<128, false>);
+        }
         return hipGetLastError();
     }
-    auto launch = [&](auto kernel, auto type, int heads) {
+    auto launch = [&](auto kernel, auto type) {
         using T = decltype(type);
-        kernel<<<dim3(pairs, unsigned(a.group / heads)), dim3(kThreads), 0, stream>>>(static_cast<const T *>(q), static_cast<const T *>(k_cache),
-                                                                                     static_cast<const T *>(v_cache), block_tables, context_lens, q_start,
-                                                                                     selected, static_cast<T *>(out), a);
+        kernel<<<grid, dim3(kThreads), 0, stream>>>(static_cast<const T *>(q), static_cast<const T *>(k_cache), static_cast<const T *>(v_cache), block_tables,
+                                                    context_lens, q_start, selected, static_cast<T *>(out), ws, a);
     };
 #define KVC_SELECTED(T, D)                                                          \
     do {                                                                            \
-        if (a.group % 4 == 0) launch(pa_selected_valu_kernel<T, D, 4>, T(), 4);     \
-        else if (a.group % 2 == 0) launch(pa_selected_valu_kernel<T, D, 2>, T(), 2); \
-        else launch(pa_selected_valu_kernel<T, D, 1>, T(), 1);                      \
+        if (a.heads_per_chunk == 4) launch(pa_selected_valu_kernel<T, D, 4>, T());  \
+        else if (a.heads_per_chunk == 2) launch(pa_selected_valu_kernel<T, D, 2>, T()); \
+        else launch(pa_selected_valu_kernel<T, D, 1>, T());                         \
     } while (0)
     if (dtype == KVC_F32) {
         if (head_dim == 64) KVC_SELECTED(float, 64); else KVC_SELECTED(float, 128);
