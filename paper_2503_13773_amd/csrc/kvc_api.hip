@@ -263,6 +263,7 @@ struct SelectedPlan {
     uint64_t ml_offset, bytes;  // of the workspace: counters, then the parts' accumulators, then their maxima and sums
 };
 constexpr int kSelectedGroups = 512;  // workgroups that few units are cut into
+constexpr int kSelectedFewUnits = 32;     // up to here workgroups of eight wavefronts
 constexpr int kSelectedManyUnits = 2048;  // from here on a wavefront takes a unit
 int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, SelectedPlan *pl) {
     const int rc = check_rows(d, total_q);
@@ -282,23 +283,23 @@ int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, 
     // units of a tile are indexed in 32 bits
     a.on_mfma = d->dtype == KVC_BF16 && d->block_size >= 4 &&
                 int64_t(d->num_pool_blocks) * d->num_kv_heads * std::max(1, d->block_size / 16) < (int64_t(1) << 31);
-    int tiles_of_a_trip;  // what a workgroup's wavefronts take at once
+    const int chunks = int(ceil_div(a.group, 16));
+    a.heads_per_chunk = a.on_mfma ? int(ceil_div(a.group, chunks)) : std::min(4, kvc::valu_head_chunk(a.group));
+    const int64_t heads = a.heads_per_chunk, units = int64_t(total_q) * a.num_kv_heads * ceil_div(a.group, heads);
+    int trip;  // tiles that a workgroup's wavefronts take at once
     if (a.on_mfma) {
         const int tile_log2 = d->head_dim == 64 ? 5 : 4;
-        const int chunks = int(ceil_div(a.group, 16));
-        a.heads_per_chunk = int(ceil_div(a.group, chunks));
         a.unit_log2 = std::min(a.block_size_log2, tile_log2);
         a.units_per_block_log2 = a.block_size_log2 - a.unit_log2;
         a.tiles = int(ceil_div(int64_t(budget) << a.block_size_log2, 1 << tile_log2));
-        tiles_of_a_trip = kvc::kWaves;
+        a.wave_per_unit = units >= kSelectedManyUnits;
+        a.waves = units <= kSelectedFewUnits ? 8 : 4;
+        trip = a.waves;
     } else {
-        a.heads_per_chunk = std::min(4, kvc::valu_head_chunk(a.group));
         a.tiles = budget;
-        tiles_of_a_trip = std::max(1, 64 >> a.block_size_log2);
+        trip = std::max(1, 64 >> a.block_size_log2);
     }
-    const int64_t heads = a.heads_per_chunk, units = int64_t(total_q) * a.num_kv_heads * ceil_div(a.group, heads);
-    a.wave_per_unit = a.on_mfma && units >= kSelectedManyUnits;
-    const int64_t most = std::min<int64_t>(kvc::kMaxSelectedParts, ceil_div(a.tiles, tiles_of_a_trip));
+    const int64_t most = std::min<int64_t>(kvc::kMaxSelectedParts, ceil_div(a.tiles, trip));
     const int64_t parts = units > 0 ? std::max<int64_t>(1, std::min<int64_t>(kSelectedGroups / units, most)) : 1;
     a.tiles_per_part = int(ceil_div(a.tiles, parts));
     a.parts = int(ceil_div(a.tiles, a.tiles_per_part));

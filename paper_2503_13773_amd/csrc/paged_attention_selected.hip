@@ -132,12 +132,14 @@ __device__ inline void attend_tile(HeadStateN<4> &st, Shape<64>::Tile &t, const 
 struct ListOf {
     const int32_t *selected, *table;
     int pos, own_block;  // position of the row, pool index of the block that holds it
-    int num_kv_heads, kvh, block_size_log2, unit_log2, units_per_block_log2, budget;
+    int num_kv_heads, kvh, block_size_log2, unit_log2, units_per_block_log2, budget, max_blocks_per_seq;
+    // The entry and what the table says at it are asked for without waiting for the row's position.
     __device__ int2 unit(int u) const {
         const int entry = u >> units_per_block_log2, in_block = u & ((1 << units_per_block_log2) - 1);
         const int b = entry < budget ? selected[entry] : -1;
+        const int named = table[min(max(b, 0), max_blocks_per_seq - 1)];
         const bool there = b >= 0 && b <= pos >> block_size_log2;
-        const int block = there ? table[b] : own_block;
+        const int block = there ? named : own_block;
         const int token = (b << block_size_log2) + (in_block << unit_log2);
         return int2{((block * num_kv_heads + kvh) << units_per_block_log2) + (there ? in_block : 0),
                     there ? min(max(pos + 1 - token, 0), 1 << unit_log2) : 0};
@@ -146,7 +148,9 @@ struct ListOf {
 
 // Tiles first, first + step, ... below `tiles` of a list's part that begins at tile0.  Whether any token counted.  A lane holds the place of
 // one unit; 64 >> units_log2 tiles are known at a time.  UNIFORM: units of 16 tokens and more, whose places are the same for all lanes.
-template <int HD, bool UNIFORM>
+// AGAIN: rows near this one read the same blocks, so loads leave them in L2 (1000 rows of chunks, 32 / 8 heads of 64: XXX us, with
+// the streaming loads of a decode step YYY).
+template <int HD, bool UNIFORM, bool AGAIN>
 __device__ inline bool attend_list(typename Shape<HD>::State &st, const bf16x8 (&qb)[Shape<HD>::kQ], const uint16_t *__restrict__ k_cache,
                                    const uint16_t *__restrict__ v_cache, const ListOf &list, float scale_log2e, int tile0, int tiles, int first, int step) {
     using TS = Shape<HD>;
@@ -192,16 +196,18 @@ __device__ inline bool attend_list(typename Shape<HD>::State &st, const bf16x8 (
                     x.limit[h] = min(max(__shfl(e.y, v_at) - ((4 * quad) & (unit_tokens - 1)), 0), 4);
                     full &= __ballot(x.limit[h] < 4) == 0;
                 }
+                auto load16 = [](const uint16_t *p) { return AGAIN ? *reinterpret_cast<const uint4 *>(p) : load16_stream(p); };
+                auto load8 = [](const uint16_t *p) { return AGAIN ? *reinterpret_cast<const uint2 *>(p) : load8_stream(p); };
                 if constexpr (HD == 128) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x.t.k[j] = load16_stream(kp + 32 * j);
+                    for (int j = 0; j < 4; ++j) x.t.k[j] = load16(kp + 32 * j);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x.t.v[j] = load16_stream(vp + j * HD);
+                    for (int j = 0; j < 4; ++j) x.t.v[j] = load16(vp + j * HD);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) x.t.k[2 * h + j] = load16_stream(kp + 32 * j);
+                    for (int j = 0; j < 2; ++j) x.t.k[2 * h + j] = load16(kp + 32 * j);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x.t.v[4 * h + j] = load8_stream(vp + j * HD);
+                    for (int j = 0; j < 4; ++j) x.t.v[4 * h + j] = load8(vp + j * HD);
                 }
             }
             x.full = full;
@@ -242,7 +248,7 @@ struct Unit {
 __device__ inline ListOf list_of(const SelectedArgs &a, const Unit &u, const int32_t *selected, const int32_t *block_tables) {
     const int32_t *table = block_tables + int64_t(u.n) * a.max_blocks_per_seq;
     return ListOf{selected + (int64_t(u.row) * a.num_kv_heads + u.kvh) * a.budget, table, u.pos, table[u.pos >> a.block_size_log2],
-                  a.num_kv_heads, u.kvh, a.block_size_log2, a.unit_log2, a.units_per_block_log2, a.budget};
+                  a.num_kv_heads, u.kvh, a.block_size_log2, a.unit_log2, a.units_per_block_log2, a.budget, a.max_blocks_per_seq};
 }
 
 // A wavefront per unit; blockIdx.x = KV head + KV heads * group of kWaves rows, so that with 8 KV heads each XCD keeps one.
@@ -264,7 +270,7 @@ __global__ __launch_bounds__(kThreads, 3) void pa_selected_wave_kernel(
     if (u.pos >= 0) {
         bf16x8 qb[TS::kQ];
         load_q_operand(qb, q + (int64_t(row) * a.num_q_heads + u.head0 + (r < u.heads ? r : 0)) * HD, quad, r < u.heads);
-        any = attend_list<HD, UNIFORM>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, 0, a.tiles, 0, 1);
+        any = attend_list<HD, UNIFORM, true>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, 0, a.tiles, 0, 1);
     }
     st.finish();
     if (r >= u.heads) return;
@@ -278,14 +284,14 @@ __global__ __launch_bounds__(kThreads, 3) void pa_selected_wave_kernel(
 }
 
 // A workgroup per part of a unit's list; blockIdx.x = KV head + KV heads * row, blockIdx.y = chunk of heads, blockIdx.z = part.
-template <int HD, bool UNIFORM>
-__global__ __launch_bounds__(kThreads, 2) void pa_selected_mfma_kernel(
+template <int HD, bool UNIFORM, bool AGAIN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void pa_selected_mfma_kernel(
     const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache, const uint16_t *__restrict__ v_cache, const int32_t *__restrict__ block_tables,
     const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start, const int32_t *__restrict__ selected, uint16_t *__restrict__ out,
     Workspace ws, SelectedArgs a) {
     using TS = Shape<HD>;
     constexpr int NV = TS::kVecs;
-    __shared__ float4 s_acc[kWaves][16 * HD / 4];
+    __shared__ float4 s_acc[WAVES][16 * HD / 4];
     __shared__ float2 s_ml[kMaxSelectedParts][16];  // of the wavefronts, then of the parts
     __shared__ int s_last;
     const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, quad = lane >> 4, r = lane & 15;
@@ -295,7 +301,7 @@ __global__ __launch_bounds__(kThreads, 2) void pa_selected_mfma_kernel(
     uint16_t *dst = out + (int64_t(row) * a.num_q_heads + u.head0) * HD;
     if (u.pos < 0) {
         if (part == 0)
-            for (int i = tid; i < u.heads * HD / 8; i += kThreads) reinterpret_cast<uint4 *>(dst)[i] = uint4{0u, 0u, 0u, 0u};
+            for (int i = tid; i < u.heads * HD / 8; i += (64 * WAVES)) reinterpret_cast<uint4 *>(dst)[i] = uint4{0u, 0u, 0u, 0u};
         return;
     }
     bf16x8 qb[TS::kQ];
@@ -303,8 +309,8 @@ __global__ __launch_bounds__(kThreads, 2) void pa_selected_mfma_kernel(
     typename TS::State st;
     st.reset();
     const int tile0 = part * a.tiles_per_part;
-    const bool any = attend_list<HD, UNIFORM>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, tile0,
-                                              min(a.tiles_per_part, a.tiles - tile0), wave, kWaves);
+    const bool any = attend_list<HD, UNIFORM, true>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, tile0,
+                                              min(a.tiles_per_part, a.tiles - tile0), wave, WAVES);
     st.finish();
     // a wavefront or part without a token says so with a maximum of -inf (with tokens it is -FLT_MAX at least)
 #pragma unroll
@@ -333,15 +339,15 @@ __global__ __launch_bounds__(kThreads, 2) void pa_selected_mfma_kernel(
         reinterpret_cast<uint2 *>(dst)[f] = M == -INFINITY ? uint2{0u, 0u} : w;
     };
     auto weight = [](float m, float M) __attribute__((always_inline)) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M); };
-    for (int f = tid; f < vecs; f += kThreads) {
+    for (int f = tid; f < vecs; f += (64 * WAVES)) {
         int head;
         const int at = place(f, &head);
         float M = -INFINITY, L = 0.f;
         float4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[w][head].x);
+        for (int w = 0; w < WAVES; ++w) M = fmaxf(M, s_ml[w][head].x);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float2 ml = s_ml[w][head];
             const float wgt = weight(ml.x, M);
             L = fmaf(wgt, ml.y, L);
@@ -365,32 +371,52 @@ __global__ __launch_bounds__(kThreads, 2) void pa_selected_mfma_kernel(
     if (!s_last) return;
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");  // the fetches stay behind the count
     if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int i = tid; i < parts * u.heads; i += kThreads) {
+    // thread (share, f) takes the parts share, share + shares, ... of vector f, the first of them beside the maxima and sums; the shares of
+    // a vector meet in LDS
+    const int shares = max(1, (64 * WAVES) / vecs), share = tid / vecs;
+    constexpr int kBatch = 4;
+    float4 y[kBatch];
+    auto fetch = [&](int at, int p0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            y[j] = load4_device_scope(acc_buf, (uint32_t(slot0 + min(p0 + j * shares, parts - 1)) * slot_vecs + at) * 16u);
+    };
+    int head0;
+    if (share < shares) fetch(place(tid - share * vecs, &head0), share);
+    for (int i = tid; i < parts * u.heads; i += (64 * WAVES)) {
         const int p = i / u.heads, head = i - p * u.heads;
         s_ml[p][head] = load2_device_scope(ml_buf, (uint32_t(slot0 + p) * 16u + head) * 8u);
     }
     __syncthreads();
-    for (int f = tid; f < vecs; f += kThreads) {
-        int head;
-        const int at = place(f, &head);
+    float4 *const s_share = &s_acc[0][0];
+    for (int f0 = 0; f0 < vecs; f0 += (64 * WAVES)) {  // more than once only for more vectors than threads, one share each then
+        const int f = shares > 1 ? tid - share * vecs : f0 + tid;
+        const bool active = share < shares && f < vecs;
+        int head = 0;
         float M = -INFINITY, L = 0.f;
         float4 x = {0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < parts; ++p) M = fmaxf(M, s_ml[p][head].x);
-        constexpr int kBatch = 8;
-        for (int p0 = 0; p0 < parts; p0 += kBatch) {
-            float4 y[kBatch];
+        if (active) {
+            const int at = place(f, &head);
+            for (int p = 0; p < parts; ++p) M = fmaxf(M, s_ml[p][head].x);
+            for (int p0 = shares > 1 ? share : 0; p0 < parts; p0 += kBatch * shares) {
+                if (p0 != share || f0 != 0) fetch(at, p0);
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) y[j] = load4_device_scope(acc_buf, (uint32_t(slot0 + min(p0 + j, parts - 1)) * slot_vecs + at) * 16u);
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-                if (p0 + j >= parts) break;
-                const float2 ml = s_ml[p0 + j][head];
-                const float wgt = weight(ml.x, M);
-                L = fmaf(wgt, ml.y, L);
-                add(x, wgt, y[j]);
+                for (int j = 0; j < kBatch; ++j) {
+                    const int p = p0 + j * shares;
+                    if (p >= parts) break;
+                    add(x, weight(s_ml[p][head].x, M), y[j]);
+                }
             }
+            for (int p = 0; p < parts; ++p) L = fmaf(weight(s_ml[p][head].x, M), s_ml[p][head].y, L);
         }
-        write_out(f, x, M, L);
+        if (shares > 1) {
+            if (active) s_share[tid] = x;
+            __syncthreads();
+            if (share == 0 && active)
+                for (int i = 1; i < shares; ++i) add(x, 1.f, s_share[i * vecs + f]);
+            if (share > 0) continue;
+        }
+        if (active) write_out(f, x, M, L);
     }
 }
 
@@ -622,9 +648,17 @@ hipError_t launch_attention_selected(const void *q, const void *k_cache, const v
             if (head_dim == 64) uniform ? launch(pa_selected_wave_kernel<64, true>) : launch(pa_selected_wave_kernel<64, false>);
             else uniform ? launch(pa_selected_wave_kernel<128, true>) : launch(pa_selected_wave_kernel<128, false>);
         } else {
-            auto launch = [&](auto kernel) { kernel<<<grid, dim3(kThreads), 0, stream>>>(qp, kp, vp, block_tables, context_lens, q_start, selected, op, ws, a); };
-            if (head_dim == 64) uniform ? launch(pa_selected_mfma_kernel<64, true>) : launch(pa_selected_mfma_kernel<64, false>);
-            else uniform ? launch(pa_selected_mfma_kernel<128, true>) : launch(pa_selected_mfma_kernel<128, false>);
+            auto launch = [&](auto kernel) {
+                kernel<<<grid, dim3(64 * a.waves), 0, stream>>>(qp, kp, vp, block_tables, context_lens, q_start, selected, op, ws, a);
+            };
+#define KVC_PARTS(HD, UNIFORM)                                                                                                     \
+    do {                                                                                                                           \
+        if (a.waves == 8) q_start ? launch(pa_selected_mfma_kernel<HD, UNIFORM, true, 8>) : launch(pa_selected_mfma_kernel<HD, UNIFORM, false, 8>); \
+        else q_start ? launch(pa_selected_mfma_kernel<HD, UNIFORM, true, 4>) : launch(pa_selected_mfma_kernel<HD, UNIFORM, false, 4>); \
+    } while (0)
+            if (head_dim == 64) { if (uniform) KVC_PARTS(64, true); else KVC_PARTS(64, false); }
+            else { if (uniform) KVC_PARTS(128, true); else KVC_PARTS(128, false); }
+#undef KVC_PARTS
         }
         return hipGetLastError();
     }
