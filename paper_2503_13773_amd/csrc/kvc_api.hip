@@ -288,10 +288,9 @@ int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, 
     const int64_t heads = a.heads_per_chunk, units = int64_t(total_q) * a.num_kv_heads * ceil_div(a.group, heads);
     int trip;  // tiles that a workgroup's wavefronts take at once
     if (a.on_mfma) {
-        const int tile_log2 = d->head_dim == 64 ? 5 : 4;
-        a.unit_log2 = std::min(a.block_size_log2, tile_log2);
+        a.unit_log2 = std::min(a.block_size_log2, 5);  // a tile is 32 tokens
         a.units_per_block_log2 = a.block_size_log2 - a.unit_log2;
-        a.tiles = int(ceil_div(int64_t(budget) << a.block_size_log2, 1 << tile_log2));
+        a.tiles = int(ceil_div(int64_t(budget) << a.block_size_log2, 32));
         a.wave_per_unit = units >= kSelectedManyUnits;
         a.waves = units <= kSelectedFewUnits ? 8 : 4;
         trip = a.waves;

@@ -22,110 +22,74 @@ using namespace mfma;
 constexpr int kWindow = 512;  // list entries whose places are held in LDS at a time (vector ALUs)
 
 // ---- bf16 on the matrix cores, up to 16 heads of a KV head (blocks of 4 tokens and more)
+//
+// A tile is 32 tokens.  With lane = 16 * quad + r:
+//   S[token][head]   = K . Q^T    per 16 tokens HD / 32 v_mfma_f32_16x16x32_bf16: lane holds scores of tokens 16 h + 4 quad + i of head r
+//   O^T[dim][head]  += V^T . P^T  per 16 dims one such product over the 32 tokens, depth slot 8 quad + 4 h + i = token 16 h + 4 quad + i,
+//                                 which is how the weights lie already; lane holds dims 16 b + 4 quad + i of head r
+// K and V rows go straight from the cache into LDS, 16 bytes a lane, into a stage that the wavefront has for itself: no barrier, and a
+// stage is filled again as soon as its operands are in registers, K of the next tile under the softmax of this one.  Which 16 bytes a
+// lane asks for makes the image free of bank conflicts: chunk c of K's row R at c ^ (R / 2 % 8) (heads of 64) or c ^ (R % 16); 32-byte
+// granule g of V's row R, which transposing reads take 16 rows at a time, at (g + R / 2) % 4 or (g + R) % 8.
+//
+// A lane's own loads in the operands' layout touch 64 lines per instruction, one per lane, and the vector cache takes one a cycle: 1000
+// rows of chunks, 32 / 8 heads of 64, 1024 tokens each: 172 us so, 387 cycles of it per tile and compute unit; through LDS 93 us.
 
-// Weights as a sum of two bf16 values, see compute_tile of head_dim 64.
-__device__ inline void split_weights(float p0, float p1, uint32_t *hi, uint32_t *lo) {
-    const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
-    *hi = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
-    *lo = pack_bf16(__builtin_fmaf(p0, 1.f + FLT_EPSILON, -__uint_as_float(u0 & 0xffff0000u)),
-                    __builtin_fmaf(p1, 1.f + FLT_EPSILON, -__uint_as_float(u1 & 0xffff0000u)));
-}
+template <int HD>
+struct Stage {
+    static constexpr int kTokens = 32, kRowBytes = HD * 2, kBytes = kTokens * kRowBytes;  // of K, and of V
+    static constexpr int kLoads = kBytes / 1024, kRows = 1024 / kRowBytes;                // instructions for each, rows of one
+    static constexpr int kChunks = kRowBytes / 16;
+    __device__ static int k_place(int row, int chunk) { return row * kRowBytes + ((chunk ^ (HD == 64 ? (row >> 1) & 7 : row & 15)) << 4); }
+    __device__ static int v_place(int row, int granule) {
+        return row * kRowBytes + (HD == 64 ? (granule + (row >> 1)) & 3 : (granule + row) & 7) * 32;
+    }
+    // where in its row the lane of a load finds what belongs at 16 bytes * lane of the kilobyte that load i fills
+    __device__ static int k_source(int lane, int i) {
+        const int row = i * kRows + lane / kChunks;
+        return ((lane % kChunks) ^ (HD == 64 ? (row >> 1) & 7 : row & 15)) << 4;
+    }
+    __device__ static int v_source(int lane, int i) {
+        const int row = i * kRows + lane / kChunks, place = lane % kChunks;
+        return (((place >> 1) - (HD == 64 ? row >> 1 : row)) & (HD == 64 ? 3 : 7)) * 32 + (place & 1) * 16;
+    }
+};
 
-// limit[h]: how many of this lane's tokens 16 h + 4 quad .. + 3 of the tile count; full: all of every lane's.
-__device__ inline void attend_tile(HeadStateN<8> &st, Shape<128>::Tile &t, const bf16x8 (&qb)[4], float scale_log2e, const int (&limit)[1], bool full) {
-    floatx4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[j]), qb[j], s, 0, 0, 0);
-    float sv[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sv[i] = s[i] * scale_log2e;
-    if (!full) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i >= limit[0]) {
-                sv[i] = -INFINITY;
-                t.v[i] = uint4{0u, 0u, 0u, 0u};
-            }
-    }
-    const float mx = lanes::max_over_rows(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])));
-    const float m_new = fmaxf(st.m, mx), alpha = __builtin_amdgcn_exp2f(st.m - m_new);
-    st.m = m_new;
-    float p[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(sv[i] - m_new);
-    st.l = fmaf(st.l, alpha, (p[0] + p[1]) + (p[2] + p[3]));
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) st.acc[e] *= alpha;
-    }
-    uint2 hi, lo;
-    split_weights(p[0], p[1], &hi.x, &lo.x);
-    split_weights(p[2], p[3], &hi.y, &lo.y);
-    const shortx4 ph = __builtin_bit_cast(shortx4, hi), pl = __builtin_bit_cast(shortx4, lo);
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        auto dword = [&](int i) { return w == 0 ? t.v[i].x : w == 1 ? t.v[i].y : w == 2 ? t.v[i].z : t.v[i].w; };
-        const uint32_t v0 = dword(0), v1 = dword(1), v2 = dword(2), v3 = dword(3);
-        const shortx4 even = __builtin_bit_cast(shortx4, uint2{__builtin_amdgcn_perm(v1, v0, 0x05040100u), __builtin_amdgcn_perm(v3, v2, 0x05040100u)});
-        const shortx4 odd = __builtin_bit_cast(shortx4, uint2{__builtin_amdgcn_perm(v1, v0, 0x07060302u), __builtin_amdgcn_perm(v3, v2, 0x07060302u)});
-        st.acc[2 * w] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(even, ph, st.acc[2 * w], 0, 0, 0);
-        st.acc[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(odd, ph, st.acc[2 * w + 1], 0, 0, 0);
-        st.acc[2 * w] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(even, pl, st.acc[2 * w], 0, 0, 0);
-        st.acc[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(odd, pl, st.acc[2 * w + 1], 0, 0, 0);
-    }
+// 16 bytes per lane from base + off to LDS at lds_addr + 16 * lane; base and lds_addr are uniform.  The compiler does not see these
+// accesses: the wavefront waits for them with wait_for_loads().  AGAIN: other wavefronts are about to read the same bytes.
+template <bool AGAIN>
+__device__ inline void load_to_lds(const unsigned char *base, uint32_t off, uint32_t lds_addr) {
+    if constexpr (AGAIN)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(off), "s"(base) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds_addr), "v"(off), "s"(base) : "memory");
 }
+template <bool AGAIN>
+__device__ inline void load_to_lds(const unsigned char *addr, uint32_t lds_addr) {
+    if constexpr (AGAIN) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(addr) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(lds_addr), "v"(addr) : "memory");
+}
+// At most N of the wavefront's loads are under way after it.  (Loads that the compiler issued in between make the wait longer, never shorter.)
+template <int N>
+__device__ inline void wait_for_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// What LDS reads come from may be overwritten after it.
+__device__ inline void wait_for_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-__device__ inline void attend_tile(HeadStateN<4> &st, Shape<64>::Tile &t, const bf16x8 (&qb)[2], float scale_log2e, const int (&limit)[2], bool full) {
-    float sv[8];
+// Softmax state of up to 16 heads in one wavefront: lane (quad, r) holds dims 16 b + 4 quad + i of head r in acc[b][i].
+template <int HD>
+struct State {
+    floatx4 acc[HD / 16];
+    float m, l;  // largest scaled score so far (base 2); sum of the weights, of this lane's tokens until finish()
+    __device__ void reset() {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        floatx4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 2; ++j) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[2 * h + j]), qb[j], s, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sv[4 * h + i] = s[i] * scale_log2e;
+        for (int b = 0; b < HD / 16; ++b) acc[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+        m = -FLT_MAX;  // not -inf: scores of -inf weigh nothing then, instead of -inf - -inf
+        l = 0.f;
     }
-    if (!full) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if ((i & 3) >= limit[i >> 2]) {
-                sv[i] = -INFINITY;
-                t.v[i] = uint2{0u, 0u};
-            }
-    }
-    const float mx = lanes::max_over_rows(fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7]))));
-    const float m_new = fmaxf(st.m, mx), alpha = __builtin_amdgcn_exp2f(st.m - m_new);
-    st.m = m_new;
-    float sum = 0.f;
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float p0 = __builtin_amdgcn_exp2f(sv[2 * i] - m_new), p1 = __builtin_amdgcn_exp2f(sv[2 * i + 1] - m_new);
-        sum += p0 + p1;
-        split_weights(p0, p1, hi + i, lo + i);
-    }
-    st.l = fmaf(st.l, alpha, sum);
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) st.acc[e] *= alpha;
-    }
-    const bf16x8 ph = __builtin_bit_cast(bf16x8, uint4{hi[0], hi[1], hi[2], hi[3]}), pl = __builtin_bit_cast(bf16x8, uint4{lo[0], lo[1], lo[2], lo[3]});
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        uint32_t d[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = w == 0 ? t.v[i].x : t.v[i].y;
-        auto pairs = [&](uint32_t which) {
-            return __builtin_bit_cast(bf16x8, uint4{__builtin_amdgcn_perm(d[1], d[0], which), __builtin_amdgcn_perm(d[3], d[2], which),
-                                                    __builtin_amdgcn_perm(d[5], d[4], which), __builtin_amdgcn_perm(d[7], d[6], which)});
-        };
-        const bf16x8 even = pairs(0x05040100u), odd = pairs(0x07060302u);
-        st.acc[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, ph, st.acc[2 * w], 0, 0, 0);
-        st.acc[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, ph, st.acc[2 * w + 1], 0, 0, 0);
-        st.acc[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pl, st.acc[2 * w], 0, 0, 0);
-        st.acc[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pl, st.acc[2 * w + 1], 0, 0, 0);
-    }
-}
+    __device__ void finish() { l = lanes::sum_over_rows(l); }
+};
 
 // Where unit u of a row's list lies (a unit is the part of a tile inside one block): its index in the pool, and how many of its tokens
 // count.  A unit of which none does lies where the row's own block is: it may be loaded.
@@ -147,24 +111,22 @@ struct ListOf {
 };
 
 // Tiles first, first + step, ... below `tiles` of a list's part that begins at tile0.  Whether any token counted.  A lane holds the place of
-// one unit; 64 >> units_log2 tiles are known at a time.  UNIFORM: units of 16 tokens and more, whose places are the same for all lanes.
-// AGAIN: rows near this one read the same blocks, so loads leave them in L2 (1000 rows of chunks, 32 / 8 heads of 64: XXX us, with
-// the streaming loads of a decode step YYY).
+// one unit; 64 >> units_log2 tiles are known at a time.  UNIFORM: the rows of a load lie in one unit (blocks of 8 tokens and more at
+// head_dim 64, all at 128).  AGAIN: rows near this one read the same blocks, so loads leave them in L2.
+// `stage`: K and V of a tile, this wavefront's own.
 template <int HD, bool UNIFORM, bool AGAIN>
-__device__ inline bool attend_list(typename Shape<HD>::State &st, const bf16x8 (&qb)[Shape<HD>::kQ], const uint16_t *__restrict__ k_cache,
-                                   const uint16_t *__restrict__ v_cache, const ListOf &list, float scale_log2e, int tile0, int tiles, int first, int step) {
-    using TS = Shape<HD>;
-    using Tile = typename TS::Tile;
-    constexpr int kSubs = TS::kTokens / 16;
-    struct Piece {
-        Tile t;
-        int limit[kSubs];
-        bool full;
-    };
+__device__ inline bool attend_list(State<HD> &st, const bf16x8 (&qb)[HD / 32], const uint16_t *__restrict__ k_cache, const uint16_t *__restrict__ v_cache,
+                                   const ListOf &list, float scale_log2e, int tile0, int tiles, int first, int step, unsigned char *stage) {
+    using G = Stage<HD>;
+    typedef short v4i16 __attribute__((ext_vector_type(4)));
+    typedef v4i16 __attribute__((address_space(3))) * lds_v4i16_ptr;
+    constexpr int kLoads = G::kLoads, kRows = G::kRows;
     const int lane = threadIdx.x & 63, quad = lane >> 4, r = lane & 15;
-    const int unit_log2 = list.unit_log2, units_log2 = TS::kTokensLog2 - unit_log2, unit_tokens = 1 << unit_log2;
-    const int k_off = (r & (unit_tokens - 1)) * HD + 8 * quad, v_off = ((4 * quad) & (unit_tokens - 1)) * HD + HD / 16 * r;
-    const size_t unit_elems = size_t(unit_tokens) * HD;
+    const int unit_log2 = list.unit_log2, units_log2 = 5 - unit_log2;
+    const uint32_t unit_bytes = uint32_t(G::kRowBytes) << unit_log2, in_rows = uint32_t(lane / G::kChunks) * G::kRowBytes;
+    unsigned char *const s_k = stage, *const s_v = stage + G::kBytes;
+    const uint32_t lds_k = uniform(int(uint32_t(reinterpret_cast<uintptr_t>(s_k)))), lds_v = lds_k + G::kBytes;
+    const unsigned char *const k_bytes = reinterpret_cast<const unsigned char *>(k_cache), *const v_bytes = reinterpret_cast<const unsigned char *>(v_cache);
     bool any = false;
     for (int from = first; from < tiles; from += step << (6 - units_log2)) {
         const int mine = from + step * (lane >> units_log2);
@@ -174,60 +136,113 @@ __device__ inline bool attend_list(typename Shape<HD>::State &st, const bf16x8 (
         if (there == 0) continue;
         any = true;
         const int count = ((63 - __builtin_clzll(there)) >> units_log2) + 1;
-        auto issue = [&](Piece &x, int i) __attribute__((always_inline)) {
-            bool full = true;
+        auto issue = [&](const unsigned char *cache, uint32_t lds, int i, auto source) __attribute__((always_inline)) {
 #pragma unroll
-            for (int h = 0; h < kSubs; ++h) {
-                const uint16_t *kp, *vp;
+            for (int j = 0; j < kLoads; ++j) {
+                const int row = j * kRows;  // of the tile, the load's first
                 if constexpr (UNIFORM) {
-                    // a unit is the tile, or (32-token tiles, blocks of 16) half of it
-                    const bool half = kSubs == 2 && units_log2 == 1;
-                    const int at = half ? 2 * i + h : i, in_unit = half ? 0 : 16 * h;
-                    const size_t base = size_t(uint32_t(__builtin_amdgcn_readlane(e.x, at))) * unit_elems + in_unit * HD;
-                    const int counts = __builtin_amdgcn_readlane(e.y, at) - in_unit;
-                    kp = k_cache + base + k_off;
-                    vp = v_cache + base + v_off;
-                    full &= counts >= 16;
-                    x.limit[h] = min(max(counts - 4 * quad, 0), 4);
+                    const uint32_t unit = __builtin_amdgcn_readlane(e.x, (i << units_log2) + (row >> unit_log2));
+                    load_to_lds<AGAIN>(cache + uint64_t(unit) * unit_bytes + uint32_t(row & ((1 << unit_log2) - 1)) * G::kRowBytes, in_rows + source(lane, j),
+                                       lds + 1024 * j);
                 } else {
-                    const int k_at = (i << units_log2) + ((16 * h + r) >> unit_log2), v_at = (i << units_log2) + ((16 * h + 4 * quad) >> unit_log2);
-                    kp = k_cache + size_t(uint32_t(__shfl(e.x, k_at))) * unit_elems + k_off;
-                    vp = v_cache + size_t(uint32_t(__shfl(e.x, v_at))) * unit_elems + v_off;
-                    x.limit[h] = min(max(__shfl(e.y, v_at) - ((4 * quad) & (unit_tokens - 1)), 0), 4);
-                    full &= __ballot(x.limit[h] < 4) == 0;
-                }
-                auto load16 = [](const uint16_t *p) { return AGAIN ? *reinterpret_cast<const uint4 *>(p) : load16_stream(p); };
-                auto load8 = [](const uint16_t *p) { return AGAIN ? *reinterpret_cast<const uint2 *>(p) : load8_stream(p); };
-                if constexpr (HD == 128) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x.t.k[j] = load16(kp + 32 * j);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x.t.v[j] = load16(vp + j * HD);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) x.t.k[2 * h + j] = load16(kp + 32 * j);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x.t.v[4 * h + j] = load8(vp + j * HD);
+                    const int mine = row + lane / G::kChunks;
+                    const uint32_t unit = __shfl(e.x, (i << units_log2) + (mine >> unit_log2));
+                    load_to_lds<AGAIN>(cache + uint64_t(unit) * unit_bytes + uint32_t(mine & ((1 << unit_log2) - 1)) * G::kRowBytes + source(lane, j), lds + 1024 * j);
                 }
             }
-            x.full = full;
         };
-        auto compute = [&](Piece &x) __attribute__((always_inline)) { attend_tile(st, x.t, qb, scale_log2e, x.limit, x.full); };
-        Piece A, B;
-        issue(A, 0);
-        int i = 0;
-        for (; i + 2 < count; i += 2) {
-            issue(B, i + 1);
-            compute(A);
-            issue(A, i + 2);
-            compute(B);
-        }
-        if (i + 1 < count) {
-            issue(B, i + 1);
-            compute(A);
-            compute(B);
-        } else {
-            compute(A);
+        auto issue_k = [&](int i) __attribute__((always_inline)) { issue(k_bytes, lds_k, i, G::k_source); };
+        auto issue_v = [&](int i) __attribute__((always_inline)) { issue(v_bytes, lds_v, i, G::v_source); };
+        // Q is waited for here: inside the loop the wait would be for the loads of tiles too
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j) asm volatile("" ::"v"(qb[j]));
+        issue_k(0);
+        issue_v(0);
+        for (int i = 0; i < count; ++i) {
+            const bool more = i + 1 < count;
+            // how many of this lane's tokens 16 h + 4 quad .. + 3 count; full: all of every lane's
+            int limit[2];
+            bool full = true;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int token = 16 * h + 4 * quad;
+                if (unit_log2 >= 4) {
+                    const int counts = __builtin_amdgcn_readlane(e.y, (i << units_log2) + ((16 * h) >> unit_log2)) - ((16 * h) & ((1 << unit_log2) - 1));
+                    full &= counts >= 16;
+                    limit[h] = min(max(counts - 4 * quad, 0), 4);
+                } else {
+                    limit[h] = min(max(__shfl(e.y, (i << units_log2) + (token >> unit_log2)) - (token & ((1 << unit_log2) - 1)), 0), 4);
+                    full &= __ballot(limit[h] < 4) == 0;
+                }
+            }
+            wait_for_loads<kLoads>();  // all but V's
+            bf16x8 ka[2][HD / 32];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < HD / 32; ++j) ka[h][j] = *reinterpret_cast<const bf16x8 *>(s_k + G::k_place(16 * h + r, 4 * j + quad));
+            wait_for_lds();
+            if (more) issue_k(i + 1);
+            float sv[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                floatx4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < HD / 32; ++j) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[h][j], qb[j], s, 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) sv[4 * h + t] = s[t] * scale_log2e;
+            }
+            if (!full) {
+#pragma unroll
+                for (int t = 0; t < 8; ++t)
+                    if ((t & 3) >= limit[t >> 2]) sv[t] = -INFINITY;
+            }
+            const float mx = lanes::max_over_rows(fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7]))));
+            const float m_new = fmaxf(st.m, mx), alpha = __builtin_amdgcn_exp2f(st.m - m_new);
+            st.m = m_new;
+            // Weights go into the product as a sum of two bf16 values (upper bits and rounded rest, 2^-16 relative), the sum takes them in fp32.
+            // The upper part is cut off and the rest made positive by 2^-23 of the weight (a factor that all weights share), so that an infinity in V
+            // keeps its sign, which a rest of 0 or of the other sign would turn into NaN.
+            float sum = 0.f;
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const float p0 = __builtin_amdgcn_exp2f(sv[2 * t] - m_new), p1 = __builtin_amdgcn_exp2f(sv[2 * t + 1] - m_new);
+                sum += p0 + p1;
+                const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+                hi[t] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
+                lo[t] = pack_bf16(__builtin_fmaf(p0, 1.f + FLT_EPSILON, -__uint_as_float(u0 & 0xffff0000u)),
+                                  __builtin_fmaf(p1, 1.f + FLT_EPSILON, -__uint_as_float(u1 & 0xffff0000u)));
+            }
+            st.l = fmaf(st.l, alpha, sum);
+            if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+                for (int b = 0; b < HD / 16; ++b) st.acc[b] *= alpha;
+            }
+            const bf16x8 ph = __builtin_bit_cast(bf16x8, uint4{hi[0], hi[1], hi[2], hi[3]}), pl = __builtin_bit_cast(bf16x8, uint4{lo[0], lo[1], lo[2], lo[3]});
+            if (more) wait_for_loads<kLoads>(); else wait_for_loads<0>();  // all but K of the next tile
+            uint2 va[HD / 16][2];  // lanes 4 k .. 4 k + 3 of a quad point at 16 dims of its token k and get a dim each of all four
+#pragma unroll
+            for (int b = 0; b < HD / 16; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    va[b][h] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(s_v + G::v_place(16 * h + 4 * quad + (r >> 2), b) + 8 * (r & 3))));
+            wait_for_lds();
+            if (more) issue_v(i + 1);
+            if (!full) {  // what does not count may hold anything
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t x = (limit[h] > 0 ? 0xffffu : 0u) | (limit[h] > 1 ? 0xffff0000u : 0u), y = (limit[h] > 2 ? 0xffffu : 0u) | (limit[h] > 3 ? 0xffff0000u : 0u);
+#pragma unroll
+                    for (int b = 0; b < HD / 16; ++b) va[b][h] = uint2{va[b][h].x & x, va[b][h].y & y};
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < HD / 16; ++b) {
+                const bf16x8 v = __builtin_bit_cast(bf16x8, uint4{va[b][0].x, va[b][0].y, va[b][1].x, va[b][1].y});
+                st.acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ph, st.acc[b], 0, 0, 0);
+                st.acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl, st.acc[b], 0, 0, 0);
+            }
         }
     }
     return any;
@@ -257,29 +272,29 @@ __global__ __launch_bounds__(kThreads, 3) void pa_selected_wave_kernel(
     const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache, const uint16_t *__restrict__ v_cache, const int32_t *__restrict__ block_tables,
     const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start, const int32_t *__restrict__ selected, uint16_t *__restrict__ out,
     SelectedArgs a) {
-    using TS = Shape<HD>;
+    __shared__ __attribute__((aligned(1024))) unsigned char s_stage[kWaves][2 * Stage<HD>::kBytes];
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, quad = lane >> 4, r = lane & 15;
     const int group = blockIdx.x / a.num_kv_heads, row = group * kWaves + wave;
     if (row >= a.total_q) return;
     const Unit u(a, q_start, context_lens, row, blockIdx.x - group * a.num_kv_heads, blockIdx.y);
     if (!u.there) return;
-    uint16_t *dst = out + (int64_t(row) * a.num_q_heads + u.head0 + r) * HD + HD / 4 * quad;
-    typename TS::State st;
+    uint16_t *dst = out + (int64_t(row) * a.num_q_heads + u.head0 + r) * HD + 4 * quad;
+    State<HD> st;
     st.reset();
     bool any = false;
     if (u.pos >= 0) {
-        bf16x8 qb[TS::kQ];
+        bf16x8 qb[HD / 32];
         load_q_operand(qb, q + (int64_t(row) * a.num_q_heads + u.head0 + (r < u.heads ? r : 0)) * HD, quad, r < u.heads);
-        any = attend_list<HD, UNIFORM, true>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, 0, a.tiles, 0, 1);
+        any = attend_list<HD, UNIFORM, true>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, 0, a.tiles, 0, 1,
+                                              s_stage[wave]);
     }
     st.finish();
     if (r >= u.heads) return;
     const float inv = 1.0f / st.l;
 #pragma unroll
-    for (int v = 0; v < TS::kVecs; v += 2) {
-        const float4 x = acc_vec(st, v), y = acc_vec(st, v + 1);
-        const uint4 w = {pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv), pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv)};
-        *reinterpret_cast<uint4 *>(dst + 4 * v) = any ? w : uint4{0u, 0u, 0u, 0u};
+    for (int b = 0; b < HD / 16; ++b) {
+        const uint2 w = {pack_bf16(st.acc[b][0] * inv, st.acc[b][1] * inv), pack_bf16(st.acc[b][2] * inv, st.acc[b][3] * inv)};
+        *reinterpret_cast<uint2 *>(dst + 16 * b) = any ? w : uint2{0u, 0u};
     }
 }
 
@@ -289,9 +304,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void pa_selected_mfma_kernel(
     const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache, const uint16_t *__restrict__ v_cache, const int32_t *__restrict__ block_tables,
     const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start, const int32_t *__restrict__ selected, uint16_t *__restrict__ out,
     Workspace ws, SelectedArgs a) {
-    using TS = Shape<HD>;
-    constexpr int NV = TS::kVecs;
-    __shared__ float4 s_acc[WAVES][16 * HD / 4];
+    // tiles while the wavefronts stream, what they and the parts exchange afterwards (a state is HD / 4 vectors of 16 heads: as large as a stage)
+    __shared__ __attribute__((aligned(1024))) unsigned char s_stage[WAVES][2 * Stage<HD>::kBytes];
+    float4 (*const s_acc)[16 * HD / 4] = reinterpret_cast<float4 (*)[16 * HD / 4]>(s_stage);
     __shared__ float2 s_ml[kMaxSelectedParts][16];  // of the wavefronts, then of the parts
     __shared__ int s_last;
     const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, quad = lane >> 4, r = lane & 15;
@@ -304,17 +319,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void pa_selected_mfma_kernel(
             for (int i = tid; i < u.heads * HD / 8; i += (64 * WAVES)) reinterpret_cast<uint4 *>(dst)[i] = uint4{0u, 0u, 0u, 0u};
         return;
     }
-    bf16x8 qb[TS::kQ];
+    bf16x8 qb[HD / 32];
     load_q_operand(qb, q + (int64_t(row) * a.num_q_heads + u.head0 + (r < u.heads ? r : 0)) * HD, quad, r < u.heads);
-    typename TS::State st;
+    State<HD> st;
     st.reset();
     const int tile0 = part * a.tiles_per_part;
     const bool any = attend_list<HD, UNIFORM, true>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, tile0,
-                                              min(a.tiles_per_part, a.tiles - tile0), wave, WAVES);
+                                              min(a.tiles_per_part, a.tiles - tile0), wave, WAVES, s_stage[wave]);
     st.finish();
     // a wavefront or part without a token says so with a maximum of -inf (with tokens it is -FLT_MAX at least)
+    __syncthreads();  // the stages are no longer needed
 #pragma unroll
-    for (int v = 0; v < NV; ++v) s_acc[wave][(v * 4 + quad) * 16 + r] = acc_vec(st, v);
+    for (int b = 0; b < HD / 16; ++b) s_acc[wave][(4 * b + quad) * 16 + r] = __builtin_bit_cast(float4, st.acc[b]);
     if (quad == 0) s_ml[wave][r] = float2{any ? st.m : -INFINITY, st.l};
     __syncthreads();
     const int vecs = u.heads * HD / 4;
@@ -324,8 +340,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void pa_selected_mfma_kernel(
     // vector f of the output: dims 4 d .. 4 d + 3 of a head
     auto place = [&](int f, int *head) __attribute__((always_inline)) {
         *head = f / (HD / 4);
-        const int d = f % (HD / 4);
-        return ((d % NV) * 4 + d / NV) * 16 + *head;  // a quad holds HD / 4 dims, NV vectors
+        return f % (HD / 4) * 16 + *head;
     };
     auto add = [](float4 &x, float w, const float4 &y) __attribute__((always_inline)) {
         x.x = fmaf(w, y.x, x.x);
@@ -641,12 +656,12 @@ hipError_t launch_attention_selected(const void *q, const void *k_cache, const v
     if (a.on_mfma) {
         const auto *qp = static_cast<const uint16_t *>(q), *kp = static_cast<const uint16_t *>(k_cache), *vp = static_cast<const uint16_t *>(v_cache);
         auto *op = static_cast<uint16_t *>(out);
-        const bool uniform = a.unit_log2 >= 4;
+        const bool uniform = head_dim == 128 || a.unit_log2 >= 3;  // the rows of a load are in one unit
         if (a.wave_per_unit) {
             const dim3 waves(unsigned((a.total_q + kWaves - 1) / kWaves) * unsigned(a.num_kv_heads), chunks);
             auto launch = [&](auto kernel) { kernel<<<waves, dim3(kThreads), 0, stream>>>(qp, kp, vp, block_tables, context_lens, q_start, selected, op, a); };
             if (head_dim == 64) uniform ? launch(pa_selected_wave_kernel<64, true>) : launch(pa_selected_wave_kernel<64, false>);
-            else uniform ? launch(pa_selected_wave_kernel<128, true>) : launch(pa_selected_wave_kernel<128, false>);
+            else launch(pa_selected_wave_kernel<128, true>);
         } else {
             auto launch = [&](auto kernel) {
                 kernel<<<grid, dim3(64 * a.waves), 0, stream>>>(qp, kp, vp, block_tables, context_lens, q_start, selected, op, ws, a);
@@ -657,7 +672,7 @@ hipError_t launch_attention_selected(const void *q, const void *k_cache, const v
         else q_start ? launch(pa_selected_mfma_kernel<HD, UNIFORM, true, 4>) : launch(pa_selected_mfma_kernel<HD, UNIFORM, false, 4>); \
     } while (0)
             if (head_dim == 64) { if (uniform) KVC_PARTS(64, true); else KVC_PARTS(64, false); }
-            else { if (uniform) KVC_PARTS(128, true); else KVC_PARTS(128, false); }
+            else KVC_PARTS(128, true);
 #undef KVC_PARTS
         }
         return hipGetLastError();

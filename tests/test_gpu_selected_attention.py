@@ -61,6 +61,23 @@ def test_rows_of_chunks(dtype, hq, hkv, d, bs):
         assert got[:2].isnan().all() and got[80:].isnan().all()
 
 
+@pytest.mark.parametrize("hq,hkv,d,bs", [(16, 8, 64, 32), (24, 8, 128, 16), (8, 8, 64, 4), (20, 4, 64, 8), (40, 2, 128, 4), (8, 8, 64, 256)])
+def test_many_rows(hq, hkv, d, bs):
+    """Enough rows for a wavefront each; rows of no sequence in front and behind, lists of any order with gaps."""
+    print(f"[case] selected many rows {hq}/{hkv} x {d} bs {bs}", flush=True)
+    rng = np.random.default_rng(hq + d)
+    rows = 2100 // hkv // (-(-hq // hkv // 16)) + 9
+    ctx = [7 * bs + 1 + rows // 2, 0, 3 * bs + rows]
+    starts = np.array([1, 1 + rows // 2, 1 + rows // 2, rows - 2])
+    tables, pool = R.scattered(rng, ctx, bs, 20 + (rows + 8 * bs) // bs)
+    q, k, v = _normal(rng, (rows, hq, d), "bf16"), _normal(rng, (pool, hkv, bs, d), "bf16"), _normal(rng, (pool, hkv, bs, d), "bf16")
+    for shuffled in (False, True):
+        selected = R.some_lists(rng, R.rows_of(ctx, starts, rows), hkv, bs, 7, shuffled)
+        selected[5] = -1
+        got = _check(q, k, v, tables, ctx, starts, selected, 0.1)
+        assert got[0].isnan().all() and got[-2:].isnan().all() and (got[5] == 0).all()
+
+
 @pytest.mark.parametrize("dtype,hq,hkv,d,rows,ctx,budget,bs", [("bf16", 32, 8, 128, 1, 30011, 128, 16), ("bf16", 64, 8, 128, 5, 9000, 200, 16),
                                                                ("bf16", 12, 12, 64, 3, 12000, 100, 32), ("f32", 16, 4, 64, 2, 9000, 260, 8),
                                                                ("bf16", 4, 1, 128, 1, 20000, 1100, 16), ("bf16", 2, 1, 64, 1, 5000, 700, 4),
