@@ -241,20 +241,40 @@ int check_rows(const kvc_attn_desc *d, int32_t total_q) {
     return total_q < 0 || int64_t(total_q) * d->num_kv_heads >= (int64_t(1) << 32) / kvc::kThreads || chunks > 65535 ? KVC_ERR_BAD_SHAPE : KVC_OK;
 }
 
+constexpr int kSelectGroups = 1024;  // workgroups that the scores of few rows are cut into
 int select_args(const kvc_attn_desc *d, int32_t total_q, int32_t budget, int32_t keep_first, int32_t keep_last, kvc::SelectArgs *a) {
     const int rc = check_rows(d, total_q);
     if (rc != KVC_OK) return rc;
     // the row's own block, which may not be full yet, is always kept
     if (budget <= 0 || keep_first < 0 || keep_last < 1 || int64_t(keep_first) + keep_last > budget) return KVC_ERR_BAD_SHAPE;
-    const int bound = bound_of(*d);
-    *a = {d->num_seqs, d->num_q_heads, d->num_kv_heads, d->num_q_heads / d->num_kv_heads, ilog2(d->block_size), d->max_blocks_per_seq, bound,
-          int(ceil_div(bound, d->block_size)), budget, keep_first, keep_last};
+    *a = {};
+    a->num_seqs = d->num_seqs;
+    a->num_q_heads = d->num_q_heads;
+    a->num_kv_heads = d->num_kv_heads;
+    a->group = d->num_q_heads / d->num_kv_heads;
+    a->block_size_log2 = ilog2(d->block_size);
+    a->max_blocks_per_seq = d->max_blocks_per_seq;
+    a->max_context_len = bound_of(*d);
+    a->total_q = total_q;
+    a->max_blocks = int(ceil_div(a->max_context_len, d->block_size));
+    a->budget = budget;
+    a->keep_first = keep_first;
+    a->keep_last = keep_last;
+    a->heads_log2 = std::min(4, ilog2(a->group));
+    const int compete = a->max_blocks - keep_first - keep_last;
+    if (a->max_blocks > budget && budget > keep_first + keep_last) {
+        // rows of chunks are scored several at a time
+        const int64_t tiles = std::max<int64_t>(1, ceil_div(total_q, total_q > d->num_seqs ? 16 >> a->heads_log2 : 1) * d->num_kv_heads);
+        const int64_t shares = std::max<int64_t>(1, std::min<int64_t>(ceil_div(compete, 64), kSelectGroups / tiles));
+        a->share = int(ceil_div(ceil_div(compete, shares), 64) * 64);
+        a->shares = int(ceil_div(compete, a->share));
+        a->stride = int(ceil_div(compete, 16) * 32);  // scores of 4 bytes, or of 8 in the same place
+    }
     return KVC_OK;
 }
-// A key for every block that a row can see, unless none competes.
+// Scores of all blocks that compete, and how large the sums behind them can be.
 size_t select_bytes(const kvc::SelectArgs &a, int32_t total_q) {
-    if (a.max_blocks <= a.budget || a.budget == a.keep_first + a.keep_last) return 0;
-    return size_t(total_q) * a.num_kv_heads * a.max_blocks * sizeof(uint64_t);
+    return size_t(total_q) * a.num_kv_heads * (a.stride + a.shares) * sizeof(float);
 }
 
 // How attention over chosen blocks is cut.  All lists are equally long as far as the host knows.
@@ -986,8 +1006,8 @@ int kvc_block_select(const void *q, const void *bounds, const int32_t *block_tab
     const size_t need = select_bytes(a, total_q);
     if (need > 0 && (!workspace || workspace_bytes < need)) return KVC_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return KVC_ERR_ALIGN;
-    const hipError_t e = kvc::launch_block_select(q, bounds, block_tables, context_lens, q_start, selected, static_cast<uint64_t *>(workspace), a, total_q,
-                                                  desc->dtype, desc->head_dim, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = kvc::launch_block_select(q, bounds, block_tables, context_lens, q_start, selected, workspace, a, desc->dtype,
+                                                  desc->head_dim, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? KVC_OK : hip_failed(e);
 }
 

@@ -142,12 +142,15 @@ hipError_t launch_cache_write(const void *k_new, const void *v_new, int64_t k_ro
 hipError_t launch_key_bounds(const void *k_cache, void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
                              const kvc_attn_desc &d, int block_size_log2, int max_query_len, hipStream_t stream);
 struct SelectArgs {
-    int num_seqs, num_q_heads, num_kv_heads, group, block_size_log2, max_blocks_per_seq, max_context_len;
-    int max_blocks;  // keys a (row, KV head) has room for: blocks of max_context_len
+    int num_seqs, num_q_heads, num_kv_heads, group, block_size_log2, max_blocks_per_seq, max_context_len, total_q;
+    int max_blocks;  // blocks of max_context_len
     int budget, keep_first, keep_last;
+    int heads_log2;  // columns of a product that a row takes: the power of two from the group up, 16 at most
+    int stride;      // scores that a (row, KV head) has room for
+    int share, shares;  // blocks that a workgroup scores (a multiple of 64), and how many shares there are; 0: nothing competes
 };
 hipError_t launch_block_select(const void *q, const void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
-                               int32_t *selected, uint64_t *keys, const SelectArgs &a, int total_q, int dtype, int head_dim, hipStream_t stream);
+                               int32_t *selected, void *workspace, const SelectArgs &a, int dtype, int head_dim, hipStream_t stream);
 constexpr int kMaxSelectedParts = 64;  // parts a list is cut into at most
 struct SelectedArgs {
     int num_seqs, num_q_heads, num_kv_heads, group, block_size_log2, max_blocks_per_seq, max_context_len, budget, total_q;
