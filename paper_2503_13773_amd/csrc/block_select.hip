@@ -141,6 +141,15 @@ constexpr float kSlack = 1.02f * (sizeof(T) == 2 ? (2 * D + 16) / 4194304.f : (6
 
 __device__ inline float max_of(float a, float b) { return a != a || a > b ? a : b; }  // NaN stays
 
+// Largest over aligned groups of 1 << log2 lanes, up to 16: all of a group get it.
+__device__ inline float over_heads(float x, int log2) {
+    if (log2 > 0) x = max_of(x, lanes::permuted<lanes::kXor1>(x));
+    if (log2 > 1) x = max_of(x, lanes::permuted<lanes::kXor2>(x));
+    if (log2 > 2) x = max_of(x, lanes::permuted<lanes::kMirror8>(x));
+    if (log2 > 3) x = max_of(x, lanes::permuted<lanes::kMirror16>(x));
+    return x;
+}
+
 // Columns of a product are heads of rows of q: `heads` of them (a power of two, the group's last head again in place of what it lacks)
 // times 16 / heads rows; GROUPS such sets of rows share the loads.  Rows of products are 16 blocks.  blockIdx.x = KV head + KV heads * tile of
 // rows (tile_rows: one of a decode step, as many as there are columns for of chunks), blockIdx.y = share of the blocks.  Writes the scores of all rows of the tile, and per row and share the largest sum of sizes.
@@ -217,10 +226,8 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
 #pragma unroll
                     for (int i = 0; i < 4; ++i) size[g] = max_of(size[g], up[g][i] - down[g][i]);
                     floatx4 best = s[g];
-                    for (int off = 1; off < 1 << a.heads_log2; off <<= 1) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) best[i] = max_of(best[i], __shfl_xor(best[i], off));
-                    }
+                    for (int i = 0; i < 4; ++i) best[i] = over_heads(best[i], a.heads_log2);
                     const int row = row0 + g * set_rows + my_row;
                     if (my_head == 0 && row < row1) {
                         float *dst = scores + (int64_t(row) * a.num_kv_heads + kvh) * a.stride + b0 - a.keep_first + 4 * quad;
@@ -235,9 +242,8 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
         }
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
-#pragma unroll
-            for (int off = 16; off < 64; off <<= 1) size[g] = max_of(size[g], __shfl_xor(size[g], off));
-            for (int off = 1; off < 1 << a.heads_log2; off <<= 1) size[g] = max_of(size[g], __shfl_xor(size[g], off));
+            size[g] = lanes::over_rows(size[g], max_of);
+            size[g] = over_heads(size[g], a.heads_log2);
             if (quad == 0) s_size[wave][g][r] = size[g];
         }
         __syncthreads();
@@ -255,281 +261,302 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
 // ---- the choice
 
 // Order of numbers as order of whole numbers.
-__device__ inline uint32_t key_of(float s) {
-    const uint32_t u = __float_as_uint(s + 0.f);  // -0 is 0
-    return u >> 31 ? ~u : u | 0x80000000u;
-}
-__device__ inline float score_of(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 __device__ inline uint64_t key_of(double s) {
     if (!__builtin_isfinite(s)) return ~uint64_t(0);
-    const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
+    const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);  // -0 is 0
     return u >> 63 ? ~u : u | uint64_t(1) << 63;
 }
 
-// Scores in 64 bits of the blocks place(0) .. place(count - 1) of a row, given to put(i, key).  Channel by channel
-// max(q lo, q hi) = (q (hi + lo) + |q| (hi - lo)) / 2, and twice the score is as good.
-template <class T, int D, class Place, class Put>
-__device__ inline void score_exactly(const T *q_heads, const T *bounds, const int32_t *table, int kvh, const SelectArgs &a, int count, Place place, Put put) {
-    constexpr int N = Load<T>::N, LR = D / N, TOGETHER = 64 / LR;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % LR;
-    for (int i0 = wave * TOGETHER; i0 < count; i0 += kWaves * TOGETHER) {
-        const int i = i0 + lane / LR;
-        const T *src = bounds + (int64_t(table[place(min(i, count - 1))]) * a.num_kv_heads + kvh) * 2 * D + c * N;
-        double sum[N], width[N];
-        Load<T>::get(*reinterpret_cast<const uint4 *>(src), sum);
-        Load<T>::get(*reinterpret_cast<const uint4 *>(src + D), width);
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const double lo = sum[k], hi = width[k];
-            sum[k] = hi + lo;
-            width[k] = hi - lo;
-        }
-        uint64_t best = 0;
-#pragma unroll 1
-        for (int h = 0; h < a.group; ++h) {
-            double x[N], s = 0.0;
-            Load<T>::get(*reinterpret_cast<const uint4 *>(q_heads + int64_t(h) * D + c * N), x);
-#pragma unroll
-            for (int k = 0; k < N; ++k) s = fma(x[k], sum[k], fma(fabs(x[k]), width[k], s));
-#pragma unroll
-            for (int off = 1; off < LR; off <<= 1) s += __shfl_xor(s, off);
-            const uint64_t key = key_of(s);
-            best = key > best ? key : best;
-        }
-        if (c == 0 && i < count) put(i, best);
-    }
+// x of another lane, both halves.
+template <int CTRL>
+__device__ inline double permuted(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, uint64_t(lanes::permuted<CTRL>(uint32_t(u >> 32))) << 32 | lanes::permuted<CTRL>(uint32_t(u)));
+}
+// Sum over aligned groups of LR lanes, 8, 16 or 32.
+template <int LR>
+__device__ inline double sum_over_lanes(double x) {
+    x += permuted<lanes::kXor1>(x);
+    x += permuted<lanes::kXor2>(x);
+    x += permuted<lanes::kMirror8>(x);
+    if constexpr (LR > 8) x += permuted<lanes::kMirror16>(x);
+    if constexpr (LR > 16) x += __shfl_xor(x, 16);
+    return x;
 }
 
-// What a workgroup shares while it chooses for one (row, KV head).
-constexpr int kBand = 512;  // blocks that it ranks by comparing each with each
-struct Choice {
-    uint32_t count[256], sums[kWaves], digit[2], before[2][kWaves], sure, band;
-    float size;
-    int wide;
-    uint64_t keys[kBand];
-    int places[kBand];
+// A block's score for one head in 64 bits, by the LR lanes of a group.  Channel by channel
+// max(q lo, q hi) = (q (hi + lo) + |q| (hi - lo)) / 2, and twice the score is as good.
+template <class T, int D>
+struct Exactly {
+    static constexpr int N = Load<T>::N, LR = D / N;
+    const T *q_heads, *bounds;  // of the row and KV head; of all blocks
+    const int32_t *table;
+    int num_kv_heads, kvh;
+    __device__ uint64_t key(int place, int h) const {
+        const int c = threadIdx.x % LR;
+        const T *src = bounds + (int64_t(table[place]) * num_kv_heads + kvh) * 2 * D + c * N;
+        double lo[N], hi[N], x[N], s = 0.0;
+        Load<T>::get(*reinterpret_cast<const uint4 *>(q_heads + int64_t(h) * D + c * N), x);
+        Load<T>::get(*reinterpret_cast<const uint4 *>(src), lo);
+        Load<T>::get(*reinterpret_cast<const uint4 *>(src + D), hi);
+#pragma unroll
+        for (int i = 0; i < N; ++i) s = fma(x[i], hi[i] + lo[i], fma(fabs(x[i]), hi[i] - lo[i], s));
+        return key_of(sum_over_lanes<LR>(s));
+    }
 };
 
-// Digit of the key at which the `left` largest of those counted in s.count end (slot 255 - digit): s.digit = slot, and how many lie above.
-__device__ inline void find_digit(Choice &s, uint32_t left) {
+constexpr int kBins = 1024;  // of the scores' range
+constexpr int kBand = 512;   // blocks that are ranked by comparing each with each
+
+// MINE: scores that a thread holds; rows with more competing blocks than THREADS * MINE are scored in 64 bits throughout.
+template <class T, int D, int THREADS, int MINE>
+__global__ __launch_bounds__(THREADS) void block_choose_kernel(const T *__restrict__ q, const T *__restrict__ bounds, const int32_t *__restrict__ block_tables,
+                                                               const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start,
+                                                               const float *__restrict__ scores, const float *__restrict__ sizes,
+                                                               uint64_t *__restrict__ all_keys, int32_t *__restrict__ selected, SelectArgs a) {
+    constexpr int WAVES = THREADS / 64;
+    __shared__ uint32_t s_bins[kBins], s_sums[WAVES], s_found[2], s_between;
+    __shared__ float s_stats[WAVES][3];
+    __shared__ uint32_t s_kept[MINE][WAVES], s_equal[MINE][WAVES];
+    __shared__ uint64_t s_keys[kBand];
+    __shared__ int s_places[kBand], s_won[kBand];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const uint32_t count = s.count[tid], incl = uint32_t(lanes::prefix_sum(int(count)));
-    if (lane == 63) s.sums[wave] = incl;
-    __syncthreads();
-    uint32_t upto = incl;
-    for (int w = 0; w < wave; ++w) upto += s.sums[w];
-    if (upto >= left && upto - count < left) {  // one thread
-        s.digit[0] = tid;
-        s.digit[1] = upto - count;
-    }
-    __syncthreads();
-}
-
-// Writes, in ascending order, the blocks below nb that are kept: what(b) = 2 kept, 1 kept if among the first `left` of these, 0 not.
-template <class What>
-__device__ inline void write_kept(Choice &s, int nb, uint32_t left, int32_t *out, What what) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    // a wavefront takes consecutive blocks
-    const int share = (nb + kThreads - 1) / kThreads * 64, from = wave * share, to = min(from + share, nb);
-    uint32_t above = 0, equal = 0;
-    for (int b = from + lane; b - lane < to; b += 64) {
-        const int x = b < to ? what(b) : 0;
-        above += __popcll(__ballot(x == 2));
-        equal += __popcll(__ballot(x == 1));
-    }
-    if (lane == 0) {
-        s.before[0][wave] = above;
-        s.before[1][wave] = equal;
-    }
-    __syncthreads();
-    above = equal = 0;
-    for (int w = 0; w < wave; ++w) {
-        above += s.before[0][w];
-        equal += s.before[1][w];
-    }
-    const uint64_t below = (uint64_t(1) << lane) - 1;
-    for (int b = from + lane; b - lane < to; b += 64) {
-        const int x = b < to ? what(b) : 0;
-        const uint64_t xs = __ballot(x == 2), ys = __ballot(x == 1);
-        const uint32_t above_me = above + __popcll(xs & below), equal_me = equal + __popcll(ys & below);
-        if (x == 2 || (x == 1 && equal_me < left)) out[above_me + min(equal_me, left)] = b;
-        above += __popcll(xs);
-        equal += __popcll(ys);
-    }
-}
-
-// CAPACITY: scores that fit in LDS; rows with more competing blocks are scored in 64 bits throughout.
-template <class T, int D, int CAPACITY>
-__global__ __launch_bounds__(kThreads) void block_choose_kernel(const T *__restrict__ q, const T *__restrict__ bounds, const int32_t *__restrict__ block_tables,
-                                                                const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start,
-                                                                const float *__restrict__ scores, const float *__restrict__ sizes, int shares,
-                                                                uint64_t *__restrict__ all_keys, int32_t *__restrict__ selected, SelectArgs a) {
-    __shared__ Choice s;
-    __shared__ uint32_t s_keys[CAPACITY];
-    const int tid = threadIdx.x, lane = tid & 63;
     const int row = blockIdx.x / a.num_kv_heads, kvh = blockIdx.x - row * a.num_kv_heads;
+    // the scores are asked for before it is known how many there are: there is room for `stride` of them
+    float x[MINE], size = 0.f;
+    const float *mine = scores + int64_t(blockIdx.x) * a.stride;
+    if (a.shares > 0) {
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) x[k] = mine[min(k * THREADS + tid, a.stride - 1)];
+        size = sizes[int64_t(blockIdx.x) * a.shares + min(tid, a.shares - 1)];
+    }
     int n, pos;
     if (!find_row(row, q_start, context_lens, a.num_seqs, a.max_context_len, &n, &pos)) return;
     int32_t *out = selected + int64_t(blockIdx.x) * a.budget;
     const int nb = pos < 0 ? 0 : (pos >> a.block_size_log2) + 1;
     if (nb <= a.budget) {
-        for (int i = tid; i < a.budget; i += kThreads) out[i] = i < nb ? i : -1;
+        for (int i = tid; i < a.budget; i += THREADS) out[i] = i < nb ? i : -1;
         return;
     }
-    const int lo = a.keep_first, compete = nb - a.keep_last - a.keep_first;  // blocks lo .. lo + compete - 1 compete
-    const uint32_t places = a.budget - a.keep_first - a.keep_last;           // for so many places: fewer than compete
-    if (places == 0) {
-        write_kept(s, nb, 0, out, [&](int b) { return b < lo || b >= lo + compete ? 2 : 0; });
-        return;
-    }
+    const int lo = a.keep_first, compete = nb - a.keep_last - lo;  // blocks lo .. lo + compete - 1 compete
+    const int places = a.budget - a.keep_last - lo;                // for so many places: fewer than compete
+    for (int i = tid; i < lo + a.keep_last; i += THREADS) out[i < lo ? i : places + i] = i < lo ? i : compete + i;
+    if (places == 0) return;
+    out += lo;
     const int32_t *table = block_tables + int64_t(n) * a.max_blocks_per_seq;
-    const T *q_heads = q + (int64_t(row) * a.num_q_heads + kvh * a.group) * D;
+    const Exactly<T, D> exactly = {q + (int64_t(row) * a.num_q_heads + kvh * a.group) * D, bounds, table, a.num_kv_heads, kvh};
+    constexpr int LR = Exactly<T, D>::LR, kTeams = THREADS / LR;
+    const int team = tid / LR;
 
-    // ---- by the scores of the matrix cores
-    bool settled = false;
-    float bottom = 0.f, top = 0.f;  // scores above top are kept, ones below bottom are not
-    uint32_t left = 0;              // places for those between
-    if (compete <= CAPACITY) {
-        if (tid == 0) {
-            s.sure = s.band = 0;
-            s.wide = 0;
-        }
-        float size = 0.f;
-        for (int i = tid; i < shares; i += kThreads) {
-            if (i * a.share >= compete) break;  // shares behind have not been written
-            size = max_of(size, sizes[int64_t(blockIdx.x) * shares + i]);
-        }
-        const float *mine = scores + int64_t(blockIdx.x) * a.stride;
-        uint32_t least = ~0u, most = 0;
-        bool finite = true;
-        for (int i = tid; i < compete; i += kThreads) {
-            const float x = mine[i];
-            finite &= __builtin_isfinite(x);
-            const uint32_t key = key_of(x);
-            s_keys[i] = key;
-            least = min(least, key);
-            most = max(most, key);
-        }
+    // Writes the kept ones of a block per thread and turn, in ascending order: what = 2 kept, 1 kept if among the first `left` of these.
+    auto write_kept = [&](auto what, int turns, int left) __attribute__((always_inline)) {
+        const uint64_t below = (uint64_t(1) << lane) - 1;
+        uint32_t kept = 0, equal = 0;  // so far
+        for (int k0 = 0; k0 < turns; k0 += MINE) {
+            uint64_t xs[MINE], ys[MINE];
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            size = max_of(size, __shfl_xor(size, off));
-            least = min(least, uint32_t(__shfl_xor(int(least), off)));
-            most = max(most, uint32_t(__shfl_xor(int(most), off)));
-        }
-        finite = __ballot(!finite) == 0;
-        const int wave = tid >> 6;
-        if (lane == 0) {
-            s.count[wave] = least;
-            s.count[4 + wave] = most;
-            s.count[8 + wave] = __float_as_uint(finite ? size : INFINITY);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            least = min(least, s.count[w]);
-            most = max(most, s.count[4 + w]);
-            const float other = __uint_as_float(s.count[8 + w]);
-            size = w == 0 ? other : max_of(size, other);
-        }
-        __syncthreads();
-        const float slack = kSlack<T, D> * size + 1e-30f;
-        if (__builtin_isfinite(size) && size < 1e30f) {
-            // the smallest kept key, to where what is left of its digits spans less than the slack
-            int bits = most == least ? 0 : 32 - __builtin_clz(most ^ least);  // that differ
-            uint32_t prefix = bits < 32 ? least >> bits << bits : 0, mask = bits < 32 ? ~0u << bits : 0;
-            left = places;
-            while (bits > 0) {
-                const int shift = max(bits - 8, 0);
-                s.count[tid] = 0;
-                __syncthreads();
-                for (int i = tid; i < compete; i += kThreads) {
-                    const uint32_t key = s_keys[i];
-                    if ((key & mask) == prefix) atomicAdd(&s.count[255 - ((key >> shift) & ((1u << (bits - shift)) - 1))], 1u);
-                }
-                __syncthreads();
-                find_digit(s, left);
-                left -= s.digit[1];
-                prefix |= (255 - s.digit[0]) << shift;
-                mask |= ((1u << (bits - shift)) - 1) << shift;
-                bits = shift;
-                __syncthreads();
-                if (score_of(prefix | ~mask) - score_of(prefix) <= slack) break;
-            }
-            bottom = score_of(prefix) - 2.f * slack;
-            top = score_of(prefix | ~mask) + 2.f * slack;
-            // those between
-            for (int i0 = 0; i0 < compete; i0 += kThreads) {
-                const int i = i0 + tid;
-                const float x = i < compete ? score_of(s_keys[i]) : -INFINITY;
-                const uint64_t sure = __ballot(x > top);
-                if (lane == 0 && sure) atomicAdd(&s.sure, uint32_t(__popcll(sure)));
-                if (x >= bottom && x <= top && i < compete) {
-                    const uint32_t at = atomicAdd(&s.band, 1u);
-                    if (at < kBand) s.places[at] = lo + i;
+            for (int k = 0; k < MINE; ++k) {
+                const int i = (k0 + k) * THREADS + tid, w = i < compete ? what(k, i) : 0;
+                xs[k] = __ballot(w == 2);
+                ys[k] = __ballot(w == 1);
+                if (lane == 0) {
+                    s_kept[k][wave] = __popcll(xs[k]);
+                    s_equal[k][wave] = __popcll(ys[k]);
                 }
             }
             __syncthreads();
-            left = places - s.sure;
-            const int between = int(s.band);
-            settled = between <= kBand;
-            if (settled && uint32_t(between) != left) {
-                score_exactly<T, D>(q_heads, bounds, table, kvh, a, between, [&](int i) { return s.places[i]; }, [&](int i, uint64_t key) { s.keys[i] = key; });
-                __syncthreads();
-                for (int i = tid; i < between; i += kThreads) {
-                    const uint64_t key = s.keys[i];
-                    const int place = s.places[i];
-                    uint32_t ahead = 0;
-                    for (int j = 0; j < between; ++j) ahead += s.keys[j] > key || (s.keys[j] == key && s.places[j] < place);
-                    // kept or not from here on: a key above or below all others
-                    s_keys[place - lo] = ahead < left ? ~0u : 0u;
+#pragma unroll
+            for (int k = 0; k < MINE; ++k) {
+                uint32_t mine_kept = kept, mine_equal = equal;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    if (w == wave) {
+                        mine_kept = kept;
+                        mine_equal = equal;
+                    }
+                    kept += s_kept[k][w];
+                    equal += s_equal[k][w];
                 }
-                __syncthreads();
-            } else if (settled) {
-                for (int i = tid; i < between; i += kThreads) s_keys[s.places[i] - lo] = ~0u;
-                __syncthreads();
+                const uint64_t bit = uint64_t(1) << lane;
+                const uint32_t at = mine_kept + __popcll(xs[k] & below), before = mine_equal + __popcll(ys[k] & below);
+                if ((xs[k] & bit) || ((ys[k] & bit) && int(before) < left)) out[at + min(int(before), left)] = lo + (k0 + k) * THREADS + tid;
+            }
+            __syncthreads();
+        }
+    };
+
+    // ---- by the scores of the matrix cores
+    if (compete <= THREADS * MINE) {
+        float least = INFINITY, most = -INFINITY;
+        bool finite = true;
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) {
+            if (k * THREADS + tid < compete) {
+                finite &= __builtin_isfinite(x[k]);
+                least = fminf(least, x[k]);
+                most = fmaxf(most, x[k]);
+            } else {
+                x[k] = -INFINITY;
             }
         }
-    }
-    if (settled) {
-        write_kept(s, nb, 0, out, [&](int b) {
-            if (b < lo || b >= lo + compete) return 2;
-            const uint32_t key = s_keys[b - lo];
-            return key == ~0u || (key != 0 && score_of(key) > top) ? 2 : 0;
-        });
-        return;
+        size = tid * a.share < compete ? size : 0.f;  // shares behind have not been written
+        for (int i = tid + THREADS; i * a.share < compete; i += THREADS) size = max_of(size, sizes[int64_t(blockIdx.x) * a.shares + i]);
+        least = lanes::over_wave(least, [](float u, float v) { return fminf(u, v); });
+        most = lanes::wave_max(most);
+        size = lanes::over_wave(size, max_of);
+        if (__ballot(!finite)) size = INFINITY;
+        if (lane == 0) {
+            s_stats[wave][0] = least;
+            s_stats[wave][1] = most;
+            s_stats[wave][2] = size;
+        }
+#pragma unroll
+        for (int i = 0; i < kBins / THREADS; ++i) s_bins[i * THREADS + tid] = 0;
+        if (tid == 0) s_between = 0;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            least = fminf(least, s_stats[w][0]);
+            most = fmaxf(most, s_stats[w][1]);
+            size = max_of(size, s_stats[w][2]);
+        }
+        if (__builtin_isfinite(size) && size < 1e30f) {
+            const float slack = kSlack<T, D> * size + 1e-30f;
+            // The last kept score lies between least and most: narrowed down to a bin of a kBins-th of that, again while that leaves many
+            // blocks and the bin is wide.  A bin holds what rounding says it holds; its borders are taken a millionth of the range wider.
+            for (;;) {
+                const float range = most - least, per_bin = kBins / range;
+                // bins from the top, scores above `most` in the first
+#pragma unroll
+                for (int k = 0; k < MINE; ++k)
+                    if (x[k] >= least) atomicAdd(&s_bins[kBins - 1 - int(fminf(fmaxf((x[k] - least) * per_bin, 0.f), float(kBins - 1)))], 1u);
+                __syncthreads();
+                constexpr int kEach = kBins / THREADS;
+                uint32_t sum = 0;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) sum += s_bins[tid * kEach + i];
+                const uint32_t incl = uint32_t(lanes::prefix_sum(int(sum)));
+                if (lane == 63) s_sums[wave] = incl;
+                __syncthreads();
+                uint32_t upto = incl - sum;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) upto += w < wave ? s_sums[w] : 0;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const uint32_t count = s_bins[tid * kEach + i];
+                    if (upto < uint32_t(places) && upto + count >= uint32_t(places)) {  // one bin
+                        s_found[0] = tid * kEach + i;
+                        s_found[1] = count;
+                    }
+                    upto += count;
+                }
+                __syncthreads();
+                const int bin = kBins - 1 - int(s_found[0]);
+                const bool many = s_found[1] > 32;
+                const float width = range * (1.f / kBins), wider = range * 1e-6f + fabsf(least) * 2.5e-7f;
+                const float bottom = least + bin * width - wider;
+                most = s_found[0] == 0 ? most : bottom + width + 2.f * wider;
+                least = bottom;
+                if (!many || !(width > slack) || s_found[0] == 0) break;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) s_bins[tid * kEach + i] = 0;
+                __syncthreads();
+            }
+            const float bottom = least - 2.f * slack, top = most + 2.f * slack;  // above top: kept, below bottom: not
+            int between[MINE], sure = 0;
+#pragma unroll
+            for (int k = 0; k < MINE; ++k) {
+                between[k] = -1;
+                sure += __popcll(__ballot(x[k] > top));
+                if (x[k] >= bottom && x[k] <= top) {
+                    between[k] = int(atomicAdd(&s_between, 1u));
+                    if (between[k] < kBand) {
+                        s_places[between[k]] = lo + k * THREADS + tid;
+                        s_keys[between[k]] = 0;
+                    }
+                }
+            }
+            if (lane == 0) s_sums[wave] = sure;
+            __syncthreads();
+            int left = places;  // for those between
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) left -= s_sums[w];
+            const int band = int(s_between);
+            if (band <= kBand) {
+                if (band != left) {
+                    // a team of LR lanes per block and head
+                    for (int i = team; i < band * a.group; i += kTeams) {
+                        const int at = i / a.group;
+                        const uint64_t key = exactly.key(s_places[at], i - at * a.group);
+                        if (tid % LR == 0) atomicMax(reinterpret_cast<unsigned long long *>(&s_keys[at]), static_cast<unsigned long long>(key));
+                    }
+                    __syncthreads();
+                    for (int i = tid; i < band; i += THREADS) {
+                        const uint64_t key = s_keys[i];
+                        const int place = s_places[i];
+                        int ahead = 0;
+                        for (int j = 0; j < band; ++j) ahead += s_keys[j] > key || (s_keys[j] == key && s_places[j] < place);
+                        s_won[i] = ahead < left;
+                    }
+                    __syncthreads();
+                }
+                write_kept([&](int k, int) { return (between[k] < 0 ? x[k] > top : band == left || s_won[between[k]]) ? 2 : 0; }, MINE, 0);
+                return;
+            }
+        }
     }
 
     // ---- all in 64 bits
     uint64_t *keys = all_keys + int64_t(blockIdx.x) * (a.stride / 2);  // where the scores were
     __syncthreads();
-    score_exactly<T, D>(q_heads, bounds, table, kvh, a, compete, [&](int i) { return lo + i; }, [&](int i, uint64_t key) { keys[i] = key; });
+    for (int i = team; i < compete; i += kTeams) {
+        uint64_t best = 0;
+#pragma unroll 1
+        for (int h = 0; h < a.group; ++h) {
+            const uint64_t key = exactly.key(lo + i, h);
+            best = key > best ? key : best;
+        }
+        if (tid % LR == 0) keys[i] = best;
+    }
     __threadfence_block();
-    __syncthreads();
     // prefix, mask: the digits of the smallest key kept; left: places for those that agree in them
     uint64_t prefix = 0, mask = 0;
-    left = places;
+    int left = places;
     for (int shift = 56; shift >= 0; shift -= 8) {
-        s.count[tid] = 0;
+        if (tid < 256) s_bins[tid] = 0;
         __syncthreads();
-        for (int i = tid; i < compete; i += kThreads) {
+        for (int i = tid; i < compete; i += THREADS) {
             const uint64_t key = keys[i];
-            if ((key & mask) == prefix) atomicAdd(&s.count[255 - (uint32_t(key >> shift) & 255)], 1u);
+            if ((key & mask) == prefix) atomicAdd(&s_bins[255 - (uint32_t(key >> shift) & 255)], 1u);
         }
         __syncthreads();
-        find_digit(s, left);
-        const uint32_t at = s.digit[0];
-        left -= s.digit[1];
+        if (tid < 256) {
+            const uint32_t count = s_bins[tid], incl = uint32_t(lanes::prefix_sum(int(count)));
+            if (lane == 63) s_sums[wave] = incl;
+            s_bins[256 + tid] = incl - count;
+        }
+        __syncthreads();
+        if (tid < 256) {
+            int before = int(s_bins[256 + tid]);
+            for (int w = 0; w < wave; ++w) before += s_sums[w];
+            if (before < left && before + int(s_bins[tid]) >= left) {  // one thread
+                s_found[0] = tid;
+                s_found[1] = before;
+            }
+        }
+        __syncthreads();
+        const uint32_t at = s_found[0];
+        left -= int(s_found[1]);
         prefix |= uint64_t(255 - at) << shift;
         mask |= uint64_t(255) << shift;
-        const uint32_t here = s.count[at];
+        const int here = int(s_bins[at]);
         __syncthreads();
         if (here == left) break;  // all that agree so far are kept
     }
-    write_kept(s, nb, left, out, [&](int b) {
-        if (b < lo || b >= lo + compete) return 2;
-        const uint64_t key = keys[b - lo] & mask;
+    write_kept([&](int, int i) {
+        const uint64_t key = keys[i] & mask;
         return key > prefix ? 2 : key == prefix ? 1 : 0;
-    });
+    }, (compete + THREADS - 1) / THREADS, left);
 }
 
 }  // namespace
@@ -538,15 +565,14 @@ hipError_t launch_block_select(const void *q, const void *bounds, const int32_t 
                                int32_t *selected, void *workspace, const SelectArgs &a, int dtype, int head_dim, hipStream_t stream) {
     const int64_t pairs = int64_t(a.total_q) * a.num_kv_heads;
     float *scores = static_cast<float *>(workspace), *sizes = scores + pairs * a.stride;
-    const int shares = a.shares;
     auto with_type = [&](auto type, auto dim) {
         using T = decltype(type);
         constexpr int D = decltype(dim)::value;
         const T *qp = static_cast<const T *>(q), *bp = static_cast<const T *>(bounds);
-        if (shares > 0) {
+        if (a.shares > 0) {
             const int set_rows = 16 >> a.heads_log2;
             auto launch = [&](auto kernel, int rows) {
-                const dim3 grid(unsigned((a.total_q + rows - 1) / rows * a.num_kv_heads), unsigned(shares));
+                const dim3 grid(unsigned((a.total_q + rows - 1) / rows * a.num_kv_heads), unsigned(a.shares));
                 kernel<<<grid, dim3(kThreads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes, a, rows);
             };
             constexpr int kMore = sizeof(T) * D > 256 ? 1 : 2;  // what the registers hold
@@ -555,11 +581,11 @@ hipError_t launch_block_select(const void *q, const void *bounds, const int32_t 
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
-        auto choose = [&](auto kernel) {
-            kernel<<<dim3(unsigned(pairs)), dim3(kThreads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes, shares,
-                                                                         static_cast<uint64_t *>(workspace), selected, a);
+        auto choose = [&](auto kernel, int threads) {
+            kernel<<<dim3(unsigned(pairs)), dim3(threads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes,
+                                                                        static_cast<uint64_t *>(workspace), selected, a);
         };
-        if (a.max_blocks <= 2048) choose(block_choose_kernel<T, D, 2048>); else choose(block_choose_kernel<T, D, 12288>);
+        if (a.max_blocks <= 2048) choose(block_choose_kernel<T, D, 256, 8>, 256); else choose(block_choose_kernel<T, D, 1024, 16>, 1024);
         return hipGetLastError();
     };
     if (dtype == KVC_F32)
