@@ -416,7 +416,9 @@ KVC_API int kvc_key_bounds_update(const void *k_cache, void *bounds, const int32
  *     sequence without tokens gets -1 throughout.
  *   - Positions at or past max_context_len are taken for the last one below it.
  *   - workspace: device memory, 256-byte aligned, kvc_block_select_workspace_bytes(desc, total_q, ...) of it (may be NULL when
- *     that is 0): scratch, needs no preparation.  Calls that share one must not overlap in time.
+ *     that is 0), with the counter header and the rules of kvc_paged_attention_decode's workspace: prepared once by
+ *     kvc_paged_attention_decode_workspace_init, and one workspace that is large enough may serve all of these calls.  Calls that
+ *     share one must not overlap in time.
  */
 KVC_API size_t kvc_block_select_workspace_bytes(const kvc_attn_desc *desc, int32_t total_q, int32_t budget, int32_t keep_first,
                                                 int32_t keep_last);

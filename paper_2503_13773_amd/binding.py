@@ -670,7 +670,8 @@ def _workspace_arg(workspace):
 def new_select_workspace(q, bounds, block_tables, budget: int, *, block_size: int, max_context_len: int = 0):
     """A workspace for block_select of these shapes (None when it needs none)."""
     desc = _select_desc(q, bounds, block_tables, block_size, max_context_len)
-    return _workspace_of(int(lib().kvc_block_select_workspace_bytes(ctypes.byref(desc), q.shape[0], int(budget), 0, 1)), q.device)
+    return _workspace_of(int(lib().kvc_block_select_workspace_bytes(ctypes.byref(desc), q.shape[0], int(budget), 0, 1)), q.device,
+                         counters=True)
 
 
 def block_select(q, bounds, block_tables, context_lens, budget: int, *, block_size: int, keep_first: int = 1, keep_last: int = 1,
@@ -695,7 +696,8 @@ def block_select(q, bounds, block_tables, context_lens, budget: int, *, block_si
     _require_together(q, bounds, block_tables, context_lens, q_start, out)
     if workspace is None:
         workspace = _workspace_of(int(lib().kvc_block_select_workspace_bytes(ctypes.byref(desc), q.shape[0], int(budget),
-                                                                             int(keep_first), int(keep_last))), q.device, stream)
+                                                                             int(keep_first), int(keep_last))), q.device, stream,
+                                  counters=True)
     ws, ws_bytes = _workspace_arg(workspace)
     _check(lib().kvc_block_select(q.data_ptr(), bounds.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(), _ptr(q_start),
                                   out.data_ptr(), int(budget), int(keep_first), int(keep_last), ctypes.byref(desc), q.shape[0],

@@ -150,16 +150,323 @@ __device__ inline float over_heads(float x, int log2) {
     return x;
 }
 
+// ---- the choice
+
+// Order of numbers as order of whole numbers.
+__device__ inline uint64_t key_of(double s) {
+    if (!__builtin_isfinite(s)) return ~uint64_t(0);
+    const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);  // -0 is 0
+    return u >> 63 ? ~u : u | uint64_t(1) << 63;
+}
+
+// x of another lane, both halves.
+template <int CTRL>
+__device__ inline double permuted(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, uint64_t(lanes::permuted<CTRL>(uint32_t(u >> 32))) << 32 | lanes::permuted<CTRL>(uint32_t(u)));
+}
+// Sum over aligned groups of LR lanes, 8, 16 or 32.
+template <int LR>
+__device__ inline double sum_over_lanes(double x) {
+    x += permuted<lanes::kXor1>(x);
+    x += permuted<lanes::kXor2>(x);
+    x += permuted<lanes::kMirror8>(x);
+    if constexpr (LR > 8) x += permuted<lanes::kMirror16>(x);
+    if constexpr (LR > 16) x += __shfl_xor(x, 16);
+    return x;
+}
+
+// A block's score for one head in 64 bits, by the LR lanes of a group.  Channel by channel
+// max(q lo, q hi) = (q (hi + lo) + |q| (hi - lo)) / 2, and twice the score is as good.
+template <class T, int D>
+struct Exactly {
+    static constexpr int N = Load<T>::N, LR = D / N;
+    const T *q_heads, *bounds;  // of the row and KV head; of all blocks
+    int num_kv_heads, kvh;
+    __device__ uint64_t key(int block, int h) const {
+        const int c = threadIdx.x % LR;
+        const T *src = bounds + (int64_t(block) * num_kv_heads + kvh) * 2 * D + c * N;
+        double lo[N], hi[N], x[N], s = 0.0;
+        Load<T>::get(*reinterpret_cast<const uint4 *>(q_heads + int64_t(h) * D + c * N), x);
+        Load<T>::get(*reinterpret_cast<const uint4 *>(src), lo);
+        Load<T>::get(*reinterpret_cast<const uint4 *>(src + D), hi);
+#pragma unroll
+        for (int i = 0; i < N; ++i) s = fma(x[i], hi[i] + lo[i], fma(fabs(x[i]), hi[i] - lo[i], s));
+        return key_of(sum_over_lanes<LR>(s));
+    }
+};
+
+constexpr int kChoiceMine = 8;  // scores that a thread holds where a workgroup of kThreads chooses
+constexpr int kBins = 1024;  // of the scores' range
+constexpr int kBand = 512;   // blocks that are ranked by comparing each with each
+
+// What a workgroup shares while it chooses.
+template <int WAVES, int MINE>
+struct Choice {
+    uint32_t bins[kBins], sums[WAVES], found[2], between;
+    float stats[WAVES][3];
+    uint32_t kept[MINE][WAVES], equal[MINE][WAVES];
+    uint64_t keys[kBand];
+    int places[kBand], blocks[kBand], won[kBand];
+};
+
+// What needs no scores: rows that keep all they see, and the blocks that are always kept.  Whether there is more to do, and then for the
+// blocks lo .. lo + compete - 1 there are `places` places, fewer than that.
+__device__ inline bool keep_the_ends(int32_t *out, int pos, const SelectArgs &a, int *compete, int *places) {
+    const int nb = pos < 0 ? 0 : (pos >> a.block_size_log2) + 1;
+    if (nb <= a.budget) {
+        for (int i = threadIdx.x; i < a.budget; i += blockDim.x) out[i] = i < nb ? i : -1;
+        return false;
+    }
+    *compete = nb - a.keep_last - a.keep_first;
+    *places = a.budget - a.keep_last - a.keep_first;
+    for (int i = threadIdx.x; i < a.keep_first + a.keep_last; i += blockDim.x)
+        out[i < a.keep_first ? i : *places + i] = i < a.keep_first ? i : *compete + i;
+    return *places > 0;
+}
+
+// The rest of a row and KV head's list.  x, blocks: scores and pool indices of blocks k * THREADS + tid of those that compete, size: the largest sum of sizes, of this thread's
+// shares.  Rows with more competing blocks than THREADS * MINE are scored in 64 bits throughout.
+template <class T, int D, int THREADS, int MINE>
+__device__ inline void choose(Choice<THREADS / 64, MINE> &s, float (&x)[MINE], const int (&blocks)[MINE], float size, int row, int kvh, int compete, int places, const T *q,
+                              const T *bounds, const int32_t *table, uint64_t *keys, int32_t *out, const SelectArgs &a) {
+    constexpr int WAVES = THREADS / 64;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, lo = a.keep_first;
+    out += lo;
+    const Exactly<T, D> exactly = {q + (int64_t(row) * a.num_q_heads + kvh * a.group) * D, bounds, a.num_kv_heads, kvh};
+    constexpr int LR = Exactly<T, D>::LR, kTeams = THREADS / LR;
+    const int team = tid / LR;
+
+    // Writes, in ascending order, the blocks of this pass over MINE * THREADS of them, from block `from` on, that are kept: what(k) = 2 kept,
+    // 1 kept if among the first `left` of these (EQUAL).  kept, equal: how many there have been before.
+    auto write_kept = [&](auto what, int from, int left, auto EQUAL, uint32_t &kept, uint32_t &equal) __attribute__((always_inline)) {
+        constexpr bool kEqual = decltype(EQUAL)::value;
+        static_assert(MINE * WAVES % 64 == 0 || MINE * WAVES <= 64, "counts of a lane");
+        uint64_t xs[MINE], ys[MINE];
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) {
+            const int w = from + k * THREADS + tid < compete ? what(k) : 0;
+            xs[k] = __ballot(w == 2);
+            ys[k] = kEqual ? __ballot(w == 1) : 0;
+            if (lane == 0) {
+                s.kept[k][wave] = __popcll(xs[k]);
+                if (kEqual) s.equal[k][wave] = __popcll(ys[k]);
+            }
+        }
+        __syncthreads();
+        // a lane sums what stands before (turn k, wavefront w) = entry k * WAVES + w, 64 entries at a time
+        const uint64_t below = (uint64_t(1) << lane) - 1, bit = uint64_t(1) << lane;
+        constexpr int kEntries = MINE * WAVES, kTurns = 64 / WAVES;
+#pragma unroll
+        for (int e0 = 0; e0 < kEntries; e0 += 64) {
+            const uint32_t mine_x = e0 + lane < kEntries ? (&s.kept[0][0])[e0 + lane] : 0, mine_y = kEqual && e0 + lane < kEntries ? (&s.equal[0][0])[e0 + lane] : 0;
+            const uint32_t sum_x = uint32_t(lanes::prefix_sum(int(mine_x))), sum_y = kEqual ? uint32_t(lanes::prefix_sum(int(mine_y))) : 0;
+#pragma unroll
+            for (int j = 0; j < kTurns; ++j) {
+                const int k = e0 / WAVES + j;
+                if (k >= MINE) break;
+                const int at = j * WAVES + wave;
+                const uint32_t x_before = kept + __builtin_amdgcn_readlane(sum_x - mine_x, at) + __popcll(xs[k] & below);
+                const uint32_t y_before = kEqual ? equal + __builtin_amdgcn_readlane(sum_y - mine_y, at) + __popcll(ys[k] & below) : 0;
+                if ((xs[k] & bit) || ((ys[k] & bit) && int(y_before) < left)) out[x_before + min(int(y_before), left)] = lo + from + k * THREADS + tid;
+            }
+            kept += __builtin_amdgcn_readlane(sum_x, 63);
+            if (kEqual) equal += __builtin_amdgcn_readlane(sum_y, 63);
+        }
+    };
+    uint32_t kept = 0, equal = 0;
+
+    // ---- by the scores of the matrix cores
+    if (compete <= THREADS * MINE) {
+        float least = INFINITY, most = -INFINITY;
+        bool finite = true;
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) {
+            if (k * THREADS + tid < compete) {
+                finite &= __builtin_isfinite(x[k]);
+                least = fminf(least, x[k]);
+                most = fmaxf(most, x[k]);
+            } else {
+                x[k] = -INFINITY;
+            }
+        }
+        least = lanes::over_wave(least, [](float u, float v) { return fminf(u, v); });
+        most = lanes::wave_max(most);
+        size = lanes::over_wave(size, max_of);
+        if (__ballot(!finite)) size = INFINITY;
+        if (lane == 0) {
+            s.stats[wave][0] = least;
+            s.stats[wave][1] = most;
+            s.stats[wave][2] = size;
+        }
+#pragma unroll
+        for (int i = 0; i < kBins / THREADS; ++i) s.bins[i * THREADS + tid] = 0;
+        if (tid == 0) s.between = 0;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            least = fminf(least, s.stats[w][0]);
+            most = fmaxf(most, s.stats[w][1]);
+            size = max_of(size, s.stats[w][2]);
+        }
+        if (__builtin_isfinite(size) && size < 1e30f) {
+            const float slack = kSlack<T, D> * size + 1e-30f;
+            // The last kept score lies between least and most: narrowed down to a bin of a kBins-th of that, again while that leaves many
+            // blocks and the bin is wide.  A bin holds what rounding says it holds; its borders are taken a millionth of the range wider.
+            for (;;) {
+                const float range = most - least, per_bin = kBins / range;
+                // bins from the top, scores above `most` in the first
+#pragma unroll
+                for (int k = 0; k < MINE; ++k)
+                    if (x[k] >= least) atomicAdd(&s.bins[kBins - 1 - int(fminf(fmaxf((x[k] - least) * per_bin, 0.f), float(kBins - 1)))], 1u);
+                __syncthreads();
+                constexpr int kEach = kBins / THREADS;
+                uint32_t sum = 0;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) sum += s.bins[tid * kEach + i];
+                const uint32_t incl = uint32_t(lanes::prefix_sum(int(sum)));
+                if (lane == 63) s.sums[wave] = incl;
+                __syncthreads();
+                uint32_t upto = incl - sum;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) upto += w < wave ? s.sums[w] : 0;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const uint32_t count = s.bins[tid * kEach + i];
+                    if (upto < uint32_t(places) && upto + count >= uint32_t(places)) {  // one bin
+                        s.found[0] = tid * kEach + i;
+                        s.found[1] = count;
+                    }
+                    upto += count;
+                }
+                __syncthreads();
+                const int bin = kBins - 1 - int(s.found[0]);
+                const bool many = s.found[1] > 32;
+                const float width = range * (1.f / kBins), wider = range * 1e-6f + fabsf(least) * 2.5e-7f;
+                const float bottom = least + bin * width - wider;
+                most = s.found[0] == 0 ? most : bottom + width + 2.f * wider;
+                least = bottom;
+                if (!many || !(width > slack) || s.found[0] == 0) break;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) s.bins[tid * kEach + i] = 0;
+                __syncthreads();
+            }
+            const float bottom = least - 2.f * slack, top = most + 2.f * slack;  // above top: kept, below bottom: not
+            int between[MINE], sure = 0;
+#pragma unroll
+            for (int k = 0; k < MINE; ++k) {
+                between[k] = -1;
+                sure += __popcll(__ballot(x[k] > top));
+                if (x[k] >= bottom && x[k] <= top) {
+                    between[k] = int(atomicAdd(&s.between, 1u));
+                    if (between[k] < kBand) {
+                        s.places[between[k]] = lo + k * THREADS + tid;
+                        s.blocks[between[k]] = blocks[k];
+                        s.keys[between[k]] = 0;
+                    }
+                }
+            }
+            if (lane == 0) s.sums[wave] = sure;
+            __syncthreads();
+            int left = places;  // for those between
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) left -= s.sums[w];
+            const int band = int(s.between);
+            if (band <= kBand) {
+                if (band != left) {
+                    // a team of LR lanes per block and head
+                    for (int i = team; i < band * a.group; i += kTeams) {
+                        const int at = i / a.group;
+                        const uint64_t key = exactly.key(s.blocks[at], i - at * a.group);
+                        if (tid % LR == 0) atomicMax(reinterpret_cast<unsigned long long *>(&s.keys[at]), static_cast<unsigned long long>(key));
+                    }
+                    __syncthreads();
+                    for (int i = tid; i < band; i += THREADS) {
+                        const uint64_t key = s.keys[i];
+                        const int place = s.places[i];
+                        int ahead = 0;
+                        for (int j = 0; j < band; ++j) ahead += s.keys[j] > key || (s.keys[j] == key && s.places[j] < place);
+                        s.won[i] = ahead < left;
+                    }
+                    __syncthreads();
+                }
+                write_kept([&](int k) { return (between[k] < 0 ? x[k] > top : band == left || s.won[between[k]]) ? 2 : 0; }, 0, 0, std::false_type(), kept, equal);
+                return;
+            }
+        }
+    }
+
+    // ---- all in 64 bits
+    __syncthreads();
+    for (int i = team; i < compete; i += kTeams) {
+        uint64_t best = 0;
+#pragma unroll 1
+        for (int h = 0; h < a.group; ++h) {
+            const uint64_t key = exactly.key(table[lo + i], h);
+            best = key > best ? key : best;
+        }
+        if (tid % LR == 0) keys[i] = best;
+    }
+    __threadfence_block();
+    // prefix, mask: the digits of the smallest key kept; left: places for those that agree in them
+    uint64_t prefix = 0, mask = 0;
+    int left = places;
+    for (int shift = 56; shift >= 0; shift -= 8) {
+        if (tid < 256) s.bins[tid] = 0;
+        __syncthreads();
+        for (int i = tid; i < compete; i += THREADS) {
+            const uint64_t key = keys[i];
+            if ((key & mask) == prefix) atomicAdd(&s.bins[255 - (uint32_t(key >> shift) & 255)], 1u);
+        }
+        __syncthreads();
+        if (tid < 256) {
+            const uint32_t count = s.bins[tid], incl = uint32_t(lanes::prefix_sum(int(count)));
+            if (lane == 63) s.sums[wave] = incl;
+            s.bins[256 + tid] = incl - count;
+        }
+        __syncthreads();
+        if (tid < 256) {
+            int before = int(s.bins[256 + tid]);
+            for (int w = 0; w < wave; ++w) before += s.sums[w];
+            if (before < left && before + int(s.bins[tid]) >= left) {  // one thread
+                s.found[0] = tid;
+                s.found[1] = before;
+            }
+        }
+        __syncthreads();
+        const uint32_t at = s.found[0];
+        left -= int(s.found[1]);
+        prefix |= uint64_t(255 - at) << shift;
+        mask |= uint64_t(255) << shift;
+        const int here = int(s.bins[at]);
+        __syncthreads();
+        if (here == left) break;  // all that agree so far are kept
+    }
+    for (int from = 0; from < compete; from += MINE * THREADS) {
+        write_kept([&](int k) {
+            const uint64_t key = keys[from + k * THREADS + tid] & mask;
+            return key > prefix ? 2 : key == prefix ? 1 : 0;
+        }, from, left, std::true_type(), kept, equal);
+        __syncthreads();
+    }
+}
+
 // Columns of a product are heads of rows of q: `heads` of them (a power of two, the group's last head again in place of what it lacks)
 // times 16 / heads rows; GROUPS such sets of rows share the loads.  Rows of products are 16 blocks.  blockIdx.x = KV head + KV heads * tile of
-// rows (tile_rows: one of a decode step, as many as there are columns for of chunks), blockIdx.y = share of the blocks.  Writes the scores of all rows of the tile, and per row and share the largest sum of sizes.
-template <class T, int D, int GROUPS>
+// rows (tile_rows: one of a decode step, as many as there are columns for of chunks), blockIdx.y = share of the blocks.  Writes the scores of all
+// rows of the tile, and per row and share the largest sum of sizes.
+// HERE (tiles of one row): the workgroup that finishes a row and KV head's last share chooses for it.  Scores and sizes travel by device-scope
+// accesses; each workgroup waits for its own and counts itself; nobody waits for anybody.
+template <class T, int D, int GROUPS, bool HERE>
 __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restrict__ q, const T *__restrict__ bounds, const int32_t *__restrict__ block_tables,
                                                                 const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start,
-                                                                float *__restrict__ scores, float *__restrict__ sizes, SelectArgs a, int tile_rows) {
+                                                                float *__restrict__ scores, float *__restrict__ sizes, int32_t *__restrict__ counters,
+                                                                int32_t *__restrict__ selected, SelectArgs a, int tile_rows) {
     constexpr int J = D / 32;
     using Op = Operand<T>;
     __shared__ float s_size[kWaves][GROUPS][16];
+    __shared__ std::conditional_t<HERE, Choice<kWaves, kChoiceMine>, int> s_choice;
+    __shared__ int s_last;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, quad = lane >> 4, r = lane & 15;
     const int tile = blockIdx.x / a.num_kv_heads, kvh = blockIdx.x - tile * a.num_kv_heads;
     const int set_rows = 16 >> a.heads_log2, my_row = r >> a.heads_log2, my_head = r & ((1 << a.heads_log2) - 1);
@@ -171,6 +478,11 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
         if (q_start) row1 = min(tile_end, q_start[n + 1]);
         pos = min(pos + (row1 - 1 - row0), a.max_context_len - 1);  // of the last row, which sees the most blocks
         const int nb = pos < 0 ? 0 : (pos >> a.block_size_log2) + 1;
+        if constexpr (HERE) {
+            int compete, places;
+            if (blockIdx.y == 0) keep_the_ends(selected + (int64_t(row0) * a.num_kv_heads + kvh) * a.budget, pos, a, &compete, &places);
+            if (nb > a.budget && int(blockIdx.y) * a.share >= nb - a.keep_last - a.keep_first) continue;
+        }
         if (nb <= a.budget) continue;
         const int first = a.keep_first + blockIdx.y * a.share, last = min(nb - a.keep_last, first + a.share);
         const int32_t *table = block_tables + int64_t(n) * a.max_blocks_per_seq;
@@ -233,9 +545,15 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
                         float *dst = scores + (int64_t(row) * a.num_kv_heads + kvh) * a.stride + b0 - a.keep_first + 4 * quad;
                         if (h0 > 0) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) best[i] = max_of(dst[i], best[i]);
+                            for (int i = 0; i < 4; ++i) best[i] = max_of(HERE ? __hip_atomic_load(dst + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : dst[i], best[i]);
                         }
-                        *reinterpret_cast<floatx4 *>(dst) = best;  // rows of `stride` have room for whole sets of blocks
+                        // rows of `stride` have room for whole sets of blocks
+                        if constexpr (HERE) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) __hip_atomic_store(dst + i, best[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        } else {
+                            *reinterpret_cast<floatx4 *>(dst) = best;
+                        }
                     }
                 }
             }
@@ -252,311 +570,66 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
             float x = s_size[0][g][r];
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) x = max_of(x, s_size[w][g][r]);
-            if (my_head == 0 && row < row1) sizes[(int64_t(row) * a.num_kv_heads + kvh) * gridDim.y + blockIdx.y] = x;
+            if (my_head == 0 && row < row1) {
+                float *dst = sizes + (int64_t(row) * a.num_kv_heads + kvh) * gridDim.y + blockIdx.y;
+                if (HERE) __hip_atomic_store(dst, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); else *dst = x;
+            }
+        }
+        if constexpr (HERE) {
+            // the count may become visible only after the scores: every wavefront waits for its own stores, then all meet
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            const int compete = nb - a.keep_last - a.keep_first, shares = (compete + a.share - 1) / a.share;
+            const int64_t pair = int64_t(row0) * a.num_kv_heads + kvh;
+            if (threadIdx.x == 0) s_last = __hip_atomic_fetch_add(counters + pair, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
+            __syncthreads();
+            if (!s_last) return;
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");  // the fetches stay behind the count
+            if (threadIdx.x == 0) __hip_atomic_store(counters + pair, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            float *mine = scores + pair * a.stride;
+            float x[kChoiceMine], most = 0.f;
+            int blocks[kChoiceMine];
+#pragma unroll
+            for (int k = 0; k < kChoiceMine; ++k) {
+                blocks[k] = table[min(a.keep_first + k * kThreads + int(threadIdx.x), nb - 1)];
+                x[k] = __hip_atomic_load(mine + min(k * kThreads + int(threadIdx.x), a.stride - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            for (int i = threadIdx.x; i < shares; i += kThreads)
+                most = max_of(most, __hip_atomic_load(sizes + pair * gridDim.y + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+            choose<T, D, kThreads, kChoiceMine>(s_choice, x, blocks, most, row0, kvh, compete, a.budget - a.keep_last - a.keep_first, q, bounds, table,
+                                                reinterpret_cast<uint64_t *>(mine), selected + pair * a.budget, a);
+            return;
         }
         __syncthreads();
     }
 }
 
-// ---- the choice
-
-// Order of numbers as order of whole numbers.
-__device__ inline uint64_t key_of(double s) {
-    if (!__builtin_isfinite(s)) return ~uint64_t(0);
-    const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);  // -0 is 0
-    return u >> 63 ? ~u : u | uint64_t(1) << 63;
-}
-
-// x of another lane, both halves.
-template <int CTRL>
-__device__ inline double permuted(double x) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    return __builtin_bit_cast(double, uint64_t(lanes::permuted<CTRL>(uint32_t(u >> 32))) << 32 | lanes::permuted<CTRL>(uint32_t(u)));
-}
-// Sum over aligned groups of LR lanes, 8, 16 or 32.
-template <int LR>
-__device__ inline double sum_over_lanes(double x) {
-    x += permuted<lanes::kXor1>(x);
-    x += permuted<lanes::kXor2>(x);
-    x += permuted<lanes::kMirror8>(x);
-    if constexpr (LR > 8) x += permuted<lanes::kMirror16>(x);
-    if constexpr (LR > 16) x += __shfl_xor(x, 16);
-    return x;
-}
-
-// A block's score for one head in 64 bits, by the LR lanes of a group.  Channel by channel
-// max(q lo, q hi) = (q (hi + lo) + |q| (hi - lo)) / 2, and twice the score is as good.
-template <class T, int D>
-struct Exactly {
-    static constexpr int N = Load<T>::N, LR = D / N;
-    const T *q_heads, *bounds;  // of the row and KV head; of all blocks
-    const int32_t *table;
-    int num_kv_heads, kvh;
-    __device__ uint64_t key(int place, int h) const {
-        const int c = threadIdx.x % LR;
-        const T *src = bounds + (int64_t(table[place]) * num_kv_heads + kvh) * 2 * D + c * N;
-        double lo[N], hi[N], x[N], s = 0.0;
-        Load<T>::get(*reinterpret_cast<const uint4 *>(q_heads + int64_t(h) * D + c * N), x);
-        Load<T>::get(*reinterpret_cast<const uint4 *>(src), lo);
-        Load<T>::get(*reinterpret_cast<const uint4 *>(src + D), hi);
-#pragma unroll
-        for (int i = 0; i < N; ++i) s = fma(x[i], hi[i] + lo[i], fma(fabs(x[i]), hi[i] - lo[i], s));
-        return key_of(sum_over_lanes<LR>(s));
-    }
-};
-
-constexpr int kBins = 1024;  // of the scores' range
-constexpr int kBand = 512;   // blocks that are ranked by comparing each with each
-
-// MINE: scores that a thread holds; rows with more competing blocks than THREADS * MINE are scored in 64 bits throughout.
+// A launch of its own, a workgroup per row and KV head.
 template <class T, int D, int THREADS, int MINE>
 __global__ __launch_bounds__(THREADS) void block_choose_kernel(const T *__restrict__ q, const T *__restrict__ bounds, const int32_t *__restrict__ block_tables,
                                                                const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start,
-                                                               const float *__restrict__ scores, const float *__restrict__ sizes,
-                                                               uint64_t *__restrict__ all_keys, int32_t *__restrict__ selected, SelectArgs a) {
-    constexpr int WAVES = THREADS / 64;
-    __shared__ uint32_t s_bins[kBins], s_sums[WAVES], s_found[2], s_between;
-    __shared__ float s_stats[WAVES][3];
-    __shared__ uint32_t s_kept[MINE][WAVES], s_equal[MINE][WAVES];
-    __shared__ uint64_t s_keys[kBand];
-    __shared__ int s_places[kBand], s_won[kBand];
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int row = blockIdx.x / a.num_kv_heads, kvh = blockIdx.x - row * a.num_kv_heads;
+                                                               float *__restrict__ scores, const float *__restrict__ sizes, int32_t *__restrict__ selected,
+                                                               SelectArgs a) {
+    __shared__ Choice<THREADS / 64, MINE> s;
+    const int tid = threadIdx.x, row = blockIdx.x / a.num_kv_heads, kvh = blockIdx.x - row * a.num_kv_heads;
     // the scores are asked for before it is known how many there are: there is room for `stride` of them
     float x[MINE], size = 0.f;
-    const float *mine = scores + int64_t(blockIdx.x) * a.stride;
+    float *mine = scores + int64_t(blockIdx.x) * a.stride;
     if (a.shares > 0) {
 #pragma unroll
         for (int k = 0; k < MINE; ++k) x[k] = mine[min(k * THREADS + tid, a.stride - 1)];
-        size = sizes[int64_t(blockIdx.x) * a.shares + min(tid, a.shares - 1)];
     }
-    int n, pos;
+    int n, pos, compete, places;
     if (!find_row(row, q_start, context_lens, a.num_seqs, a.max_context_len, &n, &pos)) return;
     int32_t *out = selected + int64_t(blockIdx.x) * a.budget;
-    const int nb = pos < 0 ? 0 : (pos >> a.block_size_log2) + 1;
-    if (nb <= a.budget) {
-        for (int i = tid; i < a.budget; i += THREADS) out[i] = i < nb ? i : -1;
-        return;
-    }
-    const int lo = a.keep_first, compete = nb - a.keep_last - lo;  // blocks lo .. lo + compete - 1 compete
-    const int places = a.budget - a.keep_last - lo;                // for so many places: fewer than compete
-    for (int i = tid; i < lo + a.keep_last; i += THREADS) out[i < lo ? i : places + i] = i < lo ? i : compete + i;
-    if (places == 0) return;
-    out += lo;
+    if (!keep_the_ends(out, pos, a, &compete, &places)) return;
     const int32_t *table = block_tables + int64_t(n) * a.max_blocks_per_seq;
-    const Exactly<T, D> exactly = {q + (int64_t(row) * a.num_q_heads + kvh * a.group) * D, bounds, table, a.num_kv_heads, kvh};
-    constexpr int LR = Exactly<T, D>::LR, kTeams = THREADS / LR;
-    const int team = tid / LR;
-
-    // Writes the kept ones of a block per thread and turn, in ascending order: what = 2 kept, 1 kept if among the first `left` of these.
-    auto write_kept = [&](auto what, int turns, int left) __attribute__((always_inline)) {
-        const uint64_t below = (uint64_t(1) << lane) - 1;
-        uint32_t kept = 0, equal = 0;  // so far
-        for (int k0 = 0; k0 < turns; k0 += MINE) {
-            uint64_t xs[MINE], ys[MINE];
+    int blocks[MINE];
 #pragma unroll
-            for (int k = 0; k < MINE; ++k) {
-                const int i = (k0 + k) * THREADS + tid, w = i < compete ? what(k, i) : 0;
-                xs[k] = __ballot(w == 2);
-                ys[k] = __ballot(w == 1);
-                if (lane == 0) {
-                    s_kept[k][wave] = __popcll(xs[k]);
-                    s_equal[k][wave] = __popcll(ys[k]);
-                }
-            }
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < MINE; ++k) {
-                uint32_t mine_kept = kept, mine_equal = equal;
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) {
-                    if (w == wave) {
-                        mine_kept = kept;
-                        mine_equal = equal;
-                    }
-                    kept += s_kept[k][w];
-                    equal += s_equal[k][w];
-                }
-                const uint64_t bit = uint64_t(1) << lane;
-                const uint32_t at = mine_kept + __popcll(xs[k] & below), before = mine_equal + __popcll(ys[k] & below);
-                if ((xs[k] & bit) || ((ys[k] & bit) && int(before) < left)) out[at + min(int(before), left)] = lo + (k0 + k) * THREADS + tid;
-            }
-            __syncthreads();
-        }
-    };
-
-    // ---- by the scores of the matrix cores
-    if (compete <= THREADS * MINE) {
-        float least = INFINITY, most = -INFINITY;
-        bool finite = true;
-#pragma unroll
-        for (int k = 0; k < MINE; ++k) {
-            if (k * THREADS + tid < compete) {
-                finite &= __builtin_isfinite(x[k]);
-                least = fminf(least, x[k]);
-                most = fmaxf(most, x[k]);
-            } else {
-                x[k] = -INFINITY;
-            }
-        }
-        size = tid * a.share < compete ? size : 0.f;  // shares behind have not been written
-        for (int i = tid + THREADS; i * a.share < compete; i += THREADS) size = max_of(size, sizes[int64_t(blockIdx.x) * a.shares + i]);
-        least = lanes::over_wave(least, [](float u, float v) { return fminf(u, v); });
-        most = lanes::wave_max(most);
-        size = lanes::over_wave(size, max_of);
-        if (__ballot(!finite)) size = INFINITY;
-        if (lane == 0) {
-            s_stats[wave][0] = least;
-            s_stats[wave][1] = most;
-            s_stats[wave][2] = size;
-        }
-#pragma unroll
-        for (int i = 0; i < kBins / THREADS; ++i) s_bins[i * THREADS + tid] = 0;
-        if (tid == 0) s_between = 0;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            least = fminf(least, s_stats[w][0]);
-            most = fmaxf(most, s_stats[w][1]);
-            size = max_of(size, s_stats[w][2]);
-        }
-        if (__builtin_isfinite(size) && size < 1e30f) {
-            const float slack = kSlack<T, D> * size + 1e-30f;
-            // The last kept score lies between least and most: narrowed down to a bin of a kBins-th of that, again while that leaves many
-            // blocks and the bin is wide.  A bin holds what rounding says it holds; its borders are taken a millionth of the range wider.
-            for (;;) {
-                const float range = most - least, per_bin = kBins / range;
-                // bins from the top, scores above `most` in the first
-#pragma unroll
-                for (int k = 0; k < MINE; ++k)
-                    if (x[k] >= least) atomicAdd(&s_bins[kBins - 1 - int(fminf(fmaxf((x[k] - least) * per_bin, 0.f), float(kBins - 1)))], 1u);
-                __syncthreads();
-                constexpr int kEach = kBins / THREADS;
-                uint32_t sum = 0;
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) sum += s_bins[tid * kEach + i];
-                const uint32_t incl = uint32_t(lanes::prefix_sum(int(sum)));
-                if (lane == 63) s_sums[wave] = incl;
-                __syncthreads();
-                uint32_t upto = incl - sum;
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) upto += w < wave ? s_sums[w] : 0;
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    const uint32_t count = s_bins[tid * kEach + i];
-                    if (upto < uint32_t(places) && upto + count >= uint32_t(places)) {  // one bin
-                        s_found[0] = tid * kEach + i;
-                        s_found[1] = count;
-                    }
-                    upto += count;
-                }
-                __syncthreads();
-                const int bin = kBins - 1 - int(s_found[0]);
-                const bool many = s_found[1] > 32;
-                const float width = range * (1.f / kBins), wider = range * 1e-6f + fabsf(least) * 2.5e-7f;
-                const float bottom = least + bin * width - wider;
-                most = s_found[0] == 0 ? most : bottom + width + 2.f * wider;
-                least = bottom;
-                if (!many || !(width > slack) || s_found[0] == 0) break;
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) s_bins[tid * kEach + i] = 0;
-                __syncthreads();
-            }
-            const float bottom = least - 2.f * slack, top = most + 2.f * slack;  // above top: kept, below bottom: not
-            int between[MINE], sure = 0;
-#pragma unroll
-            for (int k = 0; k < MINE; ++k) {
-                between[k] = -1;
-                sure += __popcll(__ballot(x[k] > top));
-                if (x[k] >= bottom && x[k] <= top) {
-                    between[k] = int(atomicAdd(&s_between, 1u));
-                    if (between[k] < kBand) {
-                        s_places[between[k]] = lo + k * THREADS + tid;
-                        s_keys[between[k]] = 0;
-                    }
-                }
-            }
-            if (lane == 0) s_sums[wave] = sure;
-            __syncthreads();
-            int left = places;  // for those between
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) left -= s_sums[w];
-            const int band = int(s_between);
-            if (band <= kBand) {
-                if (band != left) {
-                    // a team of LR lanes per block and head
-                    for (int i = team; i < band * a.group; i += kTeams) {
-                        const int at = i / a.group;
-                        const uint64_t key = exactly.key(s_places[at], i - at * a.group);
-                        if (tid % LR == 0) atomicMax(reinterpret_cast<unsigned long long *>(&s_keys[at]), static_cast<unsigned long long>(key));
-                    }
-                    __syncthreads();
-                    for (int i = tid; i < band; i += THREADS) {
-                        const uint64_t key = s_keys[i];
-                        const int place = s_places[i];
-                        int ahead = 0;
-                        for (int j = 0; j < band; ++j) ahead += s_keys[j] > key || (s_keys[j] == key && s_places[j] < place);
-                        s_won[i] = ahead < left;
-                    }
-                    __syncthreads();
-                }
-                write_kept([&](int k, int) { return (between[k] < 0 ? x[k] > top : band == left || s_won[between[k]]) ? 2 : 0; }, MINE, 0);
-                return;
-            }
-        }
-    }
-
-    // ---- all in 64 bits
-    uint64_t *keys = all_keys + int64_t(blockIdx.x) * (a.stride / 2);  // where the scores were
-    __syncthreads();
-    for (int i = team; i < compete; i += kTeams) {
-        uint64_t best = 0;
-#pragma unroll 1
-        for (int h = 0; h < a.group; ++h) {
-            const uint64_t key = exactly.key(lo + i, h);
-            best = key > best ? key : best;
-        }
-        if (tid % LR == 0) keys[i] = best;
-    }
-    __threadfence_block();
-    // prefix, mask: the digits of the smallest key kept; left: places for those that agree in them
-    uint64_t prefix = 0, mask = 0;
-    int left = places;
-    for (int shift = 56; shift >= 0; shift -= 8) {
-        if (tid < 256) s_bins[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < compete; i += THREADS) {
-            const uint64_t key = keys[i];
-            if ((key & mask) == prefix) atomicAdd(&s_bins[255 - (uint32_t(key >> shift) & 255)], 1u);
-        }
-        __syncthreads();
-        if (tid < 256) {
-            const uint32_t count = s_bins[tid], incl = uint32_t(lanes::prefix_sum(int(count)));
-            if (lane == 63) s_sums[wave] = incl;
-            s_bins[256 + tid] = incl - count;
-        }
-        __syncthreads();
-        if (tid < 256) {
-            int before = int(s_bins[256 + tid]);
-            for (int w = 0; w < wave; ++w) before += s_sums[w];
-            if (before < left && before + int(s_bins[tid]) >= left) {  // one thread
-                s_found[0] = tid;
-                s_found[1] = before;
-            }
-        }
-        __syncthreads();
-        const uint32_t at = s_found[0];
-        left -= int(s_found[1]);
-        prefix |= uint64_t(255 - at) << shift;
-        mask |= uint64_t(255) << shift;
-        const int here = int(s_bins[at]);
-        __syncthreads();
-        if (here == left) break;  // all that agree so far are kept
-    }
-    write_kept([&](int, int i) {
-        const uint64_t key = keys[i] & mask;
-        return key > prefix ? 2 : key == prefix ? 1 : 0;
-    }, (compete + THREADS - 1) / THREADS, left);
+    for (int k = 0; k < MINE; ++k) blocks[k] = table[min(a.keep_first + k * THREADS + tid, (pos >> a.block_size_log2))];
+    for (int i = tid; i * a.share < compete; i += THREADS) size = max_of(size, sizes[int64_t(blockIdx.x) * a.shares + i]);
+    choose<T, D, THREADS, MINE>(s, x, blocks, size, row, kvh, compete, places, q, bounds, table, reinterpret_cast<uint64_t *>(mine), out, a);
 }
 
 }  // namespace
@@ -564,28 +637,30 @@ __global__ __launch_bounds__(THREADS) void block_choose_kernel(const T *__restri
 hipError_t launch_block_select(const void *q, const void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
                                int32_t *selected, void *workspace, const SelectArgs &a, int dtype, int head_dim, hipStream_t stream) {
     const int64_t pairs = int64_t(a.total_q) * a.num_kv_heads;
-    float *scores = static_cast<float *>(workspace), *sizes = scores + pairs * a.stride;
+    auto *counters = static_cast<int32_t *>(workspace);
+    float *scores = reinterpret_cast<float *>(static_cast<char *>(workspace) + kWorkspaceHeaderBytes), *sizes = scores + pairs * a.stride;
     auto with_type = [&](auto type, auto dim) {
         using T = decltype(type);
         constexpr int D = decltype(dim)::value;
         const T *qp = static_cast<const T *>(q), *bp = static_cast<const T *>(bounds);
         if (a.shares > 0) {
-            const int set_rows = 16 >> a.heads_log2;
+            constexpr int kSets = select_sets(sizeof(T) == 4 ? KVC_F32 : KVC_BF16, D);
             auto launch = [&](auto kernel, int rows) {
                 const dim3 grid(unsigned((a.total_q + rows - 1) / rows * a.num_kv_heads), unsigned(a.shares));
-                kernel<<<grid, dim3(kThreads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes, a, rows);
+                kernel<<<grid, dim3(kThreads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes, counters, selected, a, rows);
             };
-            constexpr int kMore = sizeof(T) * D > 256 ? 1 : 2;  // what the registers hold
-            if (q_start && kMore > 1) launch(block_scores_kernel<T, D, kMore>, set_rows * kMore);
-            else launch(block_scores_kernel<T, D, 1>, q_start ? set_rows : 1);
+            const int set_rows = 16 >> a.heads_log2;
+            if (a.choose_here) launch(block_scores_kernel<T, D, 1, true>, 1);
+            else if (a.total_q > a.num_seqs) launch(block_scores_kernel<T, D, kSets, false>, set_rows * kSets);
+            else launch(block_scores_kernel<T, D, 1, false>, 1);
             const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
+            if (e != hipSuccess || a.choose_here) return e;
         }
-        auto choose = [&](auto kernel, int threads) {
-            kernel<<<dim3(unsigned(pairs)), dim3(threads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes,
-                                                                        static_cast<uint64_t *>(workspace), selected, a);
+        auto choose_by = [&](auto kernel, int threads) {
+            kernel<<<dim3(unsigned(pairs)), dim3(threads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes, selected, a);
         };
-        if (a.max_blocks <= 2048) choose(block_choose_kernel<T, D, 256, 8>, 256); else choose(block_choose_kernel<T, D, 1024, 16>, 1024);
+        if (a.max_blocks <= kThreads * kChoiceMine) choose_by(block_choose_kernel<T, D, kThreads, kChoiceMine>, kThreads);
+        else choose_by(block_choose_kernel<T, D, 1024, 16>, 1024);
         return hipGetLastError();
     };
     if (dtype == KVC_F32)

@@ -241,7 +241,8 @@ int check_rows(const kvc_attn_desc *d, int32_t total_q) {
     return total_q < 0 || int64_t(total_q) * d->num_kv_heads >= (int64_t(1) << 32) / kvc::kThreads || chunks > 65535 ? KVC_ERR_BAD_SHAPE : KVC_OK;
 }
 
-constexpr int kSelectGroups = 1024;  // workgroups that the scores of few rows are cut into
+constexpr int kSelectHereBlocks = 2048;  // what a workgroup of the scores can choose among
+constexpr int kSelectGroups = 2048;  // workgroups that the scores of few rows are cut into
 int select_args(const kvc_attn_desc *d, int32_t total_q, int32_t budget, int32_t keep_first, int32_t keep_last, kvc::SelectArgs *a) {
     const int rc = check_rows(d, total_q);
     if (rc != KVC_OK) return rc;
@@ -264,17 +265,19 @@ int select_args(const kvc_attn_desc *d, int32_t total_q, int32_t budget, int32_t
     const int compete = a->max_blocks - keep_first - keep_last;
     if (a->max_blocks > budget && budget > keep_first + keep_last) {
         // rows of chunks are scored several at a time
-        const int64_t tiles = std::max<int64_t>(1, ceil_div(total_q, total_q > d->num_seqs ? 16 >> a->heads_log2 : 1) * d->num_kv_heads);
+        const int64_t tiles = std::max<int64_t>(1, ceil_div(total_q, total_q > d->num_seqs ? kvc::select_sets(d->dtype, d->head_dim) * (16 >> a->heads_log2) : 1) * d->num_kv_heads);
         const int64_t shares = std::max<int64_t>(1, std::min<int64_t>(ceil_div(compete, 64), kSelectGroups / tiles));
         a->share = int(ceil_div(ceil_div(compete, shares), 64) * 64);
         a->shares = int(ceil_div(compete, a->share));
         a->stride = int(ceil_div(compete, 16) * 32);  // scores of 4 bytes, or of 8 in the same place
+        a->choose_here = total_q <= d->num_seqs && int64_t(total_q) * d->num_kv_heads <= int64_t(kvc::kWorkspaceHeaderBytes / sizeof(int32_t)) &&
+                         a->max_blocks <= kSelectHereBlocks;
     }
     return KVC_OK;
 }
-// Scores of all blocks that compete, and how large the sums behind them can be.
+// Counters, scores of all blocks that compete, and how large the sums behind them can be.
 size_t select_bytes(const kvc::SelectArgs &a, int32_t total_q) {
-    return size_t(total_q) * a.num_kv_heads * (a.stride + a.shares) * sizeof(float);
+    return a.shares == 0 || total_q == 0 ? 0 : kvc::kWorkspaceHeaderBytes + size_t(total_q) * a.num_kv_heads * (a.stride + a.shares) * sizeof(float);
 }
 
 // How attention over chosen blocks is cut.  All lists are equally long as far as the host knows.

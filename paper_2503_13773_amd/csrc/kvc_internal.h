@@ -148,7 +148,10 @@ struct SelectArgs {
     int heads_log2;  // columns of a product that a row takes: the power of two from the group up, 16 at most
     int stride;      // scores that a (row, KV head) has room for
     int share, shares;  // blocks that a workgroup scores (a multiple of 64), and how many shares there are; 0: nothing competes
+    int choose_here;    // the workgroup that scores a row's last share chooses (1), or a launch of its own does (0)
 };
+// Sets of 16 columns (heads of rows of chunks) that share the loads of bounds: what the registers hold.
+constexpr int select_sets(int dtype, int head_dim) { return dtype == KVC_F32 && head_dim == 128 ? 1 : 2; }
 hipError_t launch_block_select(const void *q, const void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
                                int32_t *selected, void *workspace, const SelectArgs &a, int dtype, int head_dim, hipStream_t stream);
 constexpr int kMaxSelectedParts = 64;  // parts a list is cut into at most

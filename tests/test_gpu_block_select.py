@@ -118,8 +118,11 @@ def test_a_bound_on_the_lengths_and_workspaces():
     small = K.new_select_workspace(q.cuda(), bounds.cuda(), torch.from_numpy(tables).cuda(), 9, block_size=bs, max_context_len=800)
     large = K.new_select_workspace(q.cuda(), bounds.cuda(), torch.from_numpy(tables).cuda(), 9, block_size=bs)
     assert small.numel() < large.numel()
-    a = _check(q, bounds, tables, ctx, None, bs, 9, 1, 2, workspace=small.fill_(255), max_context_len=800)
-    b = _check(q, bounds, tables, ctx, None, bs, 9, 1, 2, workspace=large.fill_(255))
+    small[4096:].fill_(255)   # behind the counters anything may stand
+    large[4096:].fill_(255)
+    a = _check(q, bounds, tables, ctx, None, bs, 9, 1, 2, workspace=small, max_context_len=800)
+    b = _check(q, bounds, tables, ctx, None, bs, 9, 1, 2, workspace=large)
+    assert not small[:4096].any() and not large[:4096].any()
     assert np.array_equal(a, b)
     with pytest.raises(K.KvcError) as e:
         _check(q, bounds, tables, ctx, None, bs, 9, 1, 2, workspace=small)
