@@ -582,11 +582,11 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
             __syncthreads();
             const int compete = nb - a.keep_last - a.keep_first, shares = (compete + a.share - 1) / a.share;
             const int64_t pair = int64_t(row0) * a.num_kv_heads + kvh;
-            if (threadIdx.x == 0) s_last = __hip_atomic_fetch_add(counters + pair, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
+            if (threadIdx.x == 0) s_last = __hip_atomic_fetch_add(counters + pair * a.counter_step, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
             __syncthreads();
             if (!s_last) return;
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");  // the fetches stay behind the count
-            if (threadIdx.x == 0) __hip_atomic_store(counters + pair, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (threadIdx.x == 0) __hip_atomic_store(counters + pair * a.counter_step, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             float *mine = scores + pair * a.stride;
             float x[kChoiceMine], most = 0.f;
             int blocks[kChoiceMine];

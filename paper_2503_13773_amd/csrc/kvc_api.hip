@@ -270,6 +270,7 @@ int select_args(const kvc_attn_desc *d, int32_t total_q, int32_t budget, int32_t
         a->share = int(ceil_div(ceil_div(compete, shares), 64) * 64);
         a->shares = int(ceil_div(compete, a->share));
         a->stride = int(ceil_div(compete, 16) * 32);  // scores of 4 bytes, or of 8 in the same place
+        a->counter_step = kvc::counter_step(int64_t(total_q) * d->num_kv_heads);
         a->choose_here = total_q <= d->num_seqs && int64_t(total_q) * d->num_kv_heads <= int64_t(kvc::kWorkspaceHeaderBytes / sizeof(int32_t)) &&
                          a->max_blocks <= kSelectHereBlocks;
     }
@@ -326,6 +327,7 @@ int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, 
     a.tiles_per_part = int(ceil_div(a.tiles, parts));
     a.parts = int(ceil_div(a.tiles, a.tiles_per_part));
     pl->ml_offset = pl->bytes = 0;
+    a.counter_step = kvc::counter_step(units);
     if (a.parts > 1) {
         const uint64_t slots = uint64_t(units) * a.parts, slot_heads = a.on_mfma ? 16 : heads;
         pl->ml_offset = kvc::kWorkspaceHeaderBytes + slots * slot_heads * d->head_dim * sizeof(float);

@@ -141,6 +141,13 @@ hipError_t launch_cache_write(const void *k_new, const void *v_new, int64_t k_ro
                               int64_t num_slots, hipStream_t stream);
 hipError_t launch_key_bounds(const void *k_cache, void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
                              const kvc_attn_desc &d, int block_size_log2, int max_query_len, hipStream_t stream);
+// Counters of few rows are spread over the workspace's header: those on one line are counted one after the other, whatever XCD they come
+// from (one request, 32 / 8 heads, 30 workgroups for each of 8 counters side by side: 2 us from the store of a part to the count).
+inline int counter_step(int64_t counters) {
+    int step = 1;
+    while (2 * step * counters <= int64_t(kWorkspaceHeaderBytes / sizeof(int32_t)) && step < 32) step *= 2;
+    return step;
+}
 struct SelectArgs {
     int num_seqs, num_q_heads, num_kv_heads, group, block_size_log2, max_blocks_per_seq, max_context_len, total_q;
     int max_blocks;  // blocks of max_context_len
@@ -148,6 +155,7 @@ struct SelectArgs {
     int heads_log2;  // columns of a product that a row takes: the power of two from the group up, 16 at most
     int stride;      // scores that a (row, KV head) has room for
     int share, shares;  // blocks that a workgroup scores (a multiple of 64), and how many shares there are; 0: nothing competes
+    int counter_step;   // counters of (row, KV head) pairs lie so many words apart
     int choose_here;    // the workgroup that scores a row's last share chooses (1), or a launch of its own does (0)
 };
 // Sets of 16 columns (heads of rows of chunks) that share the loads of bounds: what the registers hold.
@@ -160,6 +168,7 @@ struct SelectedArgs {
     float scale, scale_log2e;
     // how the work is cut: wavefronts of a workgroup, heads of a KV head in a unit, tiles of a list (vector ALUs: entries), parts of a list and tiles of one
     int on_mfma, wave_per_unit, waves, heads_per_chunk, unit_log2, units_per_block_log2, tiles, parts, tiles_per_part;
+    int counter_step;  // counters of units lie so many words apart
 };
 hipError_t launch_attention_selected(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables, const int32_t *context_lens,
                                      const int32_t *q_start, const int32_t *selected, void *out, Workspace ws, const SelectedArgs &a, int dtype,

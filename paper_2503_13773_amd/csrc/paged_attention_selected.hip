@@ -380,7 +380,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void pa_selected_mfma_kernel(
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    int32_t *const counter = ws.cnt + blockIdx.x * gridDim.y + blockIdx.y;
+    int32_t *const counter = ws.cnt + (blockIdx.x * gridDim.y + blockIdx.y) * a.counter_step;
     if (tid == 0) s_last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
     __syncthreads();
     if (!s_last) return;
@@ -615,11 +615,11 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");  // as above
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tid == 0) s_last = __hip_atomic_fetch_add(ws.cnt + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+    if (tid == 0) s_last = __hip_atomic_fetch_add(ws.cnt + unit * a.counter_step, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
     __syncthreads();
     if (!s_last) return;
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
-    if (tid == 0) __hip_atomic_store(ws.cnt + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid == 0) __hip_atomic_store(ws.cnt + unit * a.counter_step, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     for (int i = tid; i < parts * HEADS; i += kThreads) {
         s_m[i / HEADS][i % HEADS] = load_device(ws.ml + (slot0 * HEADS + i) * 2);
         s_l[i / HEADS][i % HEADS] = load_device(ws.ml + (slot0 * HEADS + i) * 2 + 1);
