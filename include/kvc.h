@@ -366,7 +366,7 @@ typedef struct {
  *   - it lacks blocks and they, with those that the sequences before it ask for (granted or not), exceed num_free;
  *   - its new tokens, with those of the sequences before it (granted or not), exceed max_rows.
  * The sequences behind go by the same rules, so what is taken is always the front of free_blocks.  A new token whose table
- * entry is negative gets slot -1.  No output may overlap another array of the call (KVC_ERR_OVERLAP).  Up to 4096 sequences one launch,
+ * entry is negative gets slot -1.  No output may overlap another array of the call (KVC_ERR_OVERLAP).  Up to 2048 sequences one launch,
  * above two.  With num_seqs == 0 the maps are filled with -1.
  */
 KVC_API int kvc_block_tables_extend(int32_t *block_tables, const int32_t *context_lens, const int32_t *new_lens,

@@ -197,12 +197,12 @@ struct Exactly {
 };
 
 constexpr int kChoiceMine = 8;  // scores that a thread holds where a workgroup of kThreads chooses
-constexpr int kBins = 1024;  // of the scores' range
-constexpr int kBand = 512;   // blocks that are ranked by comparing each with each
 
 // What a workgroup shares while it chooses.
 template <int WAVES, int MINE>
 struct Choice {
+    static constexpr int kBins = WAVES == 1 ? 256 : 1024;  // of the scores' range
+    static constexpr int kBand = WAVES == 1 ? 128 : 512;   // blocks that are ranked by comparing each with each
     uint32_t bins[kBins], sums[WAVES], found[2], between;
     float stats[WAVES][3];
     uint32_t kept[MINE][WAVES], equal[MINE][WAVES];
@@ -230,7 +230,7 @@ __device__ inline bool keep_the_ends(int32_t *out, int pos, const SelectArgs &a,
 template <class T, int D, int THREADS, int MINE>
 __device__ inline void choose(Choice<THREADS / 64, MINE> &s, float (&x)[MINE], const int (&blocks)[MINE], float size, int row, int kvh, int compete, int places, const T *q,
                               const T *bounds, const int32_t *table, uint64_t *keys, int32_t *out, const SelectArgs &a) {
-    constexpr int WAVES = THREADS / 64;
+    constexpr int WAVES = THREADS / 64, kBins = Choice<WAVES, MINE>::kBins, kBand = Choice<WAVES, MINE>::kBand;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, lo = a.keep_first;
     out += lo;
     const Exactly<T, D> exactly = {q + (int64_t(row) * a.num_q_heads + kvh * a.group) * D, bounds, a.num_kv_heads, kvh};
@@ -411,24 +411,28 @@ __device__ inline void choose(Choice<THREADS / 64, MINE> &s, float (&x)[MINE], c
     // prefix, mask: the digits of the smallest key kept; left: places for those that agree in them
     uint64_t prefix = 0, mask = 0;
     int left = places;
-    for (int shift = 56; shift >= 0; shift -= 8) {
-        if (tid < 256) s.bins[tid] = 0;
+    constexpr int kDigit = THREADS < 256 ? 6 : 8, kDigits = 1 << kDigit;
+    for (int bits = 64; bits > 0;) {
+        const int shift = max(bits - kDigit, 0);
+        const uint32_t last = (1u << (bits - shift)) - 1;
+        if (tid < kDigits) s.bins[tid] = 0;
         __syncthreads();
         for (int i = tid; i < compete; i += THREADS) {
             const uint64_t key = keys[i];
-            if ((key & mask) == prefix) atomicAdd(&s.bins[255 - (uint32_t(key >> shift) & 255)], 1u);
+            if ((key & mask) == prefix) atomicAdd(&s.bins[last - (uint32_t(key >> shift) & last)], 1u);
         }
         __syncthreads();
-        if (tid < 256) {
-            const uint32_t count = s.bins[tid], incl = uint32_t(lanes::prefix_sum(int(count)));
+        uint32_t count = 0, incl = 0;
+        if (tid < kDigits) {
+            count = s.bins[tid];
+            incl = uint32_t(lanes::prefix_sum(int(count)));
             if (lane == 63) s.sums[wave] = incl;
-            s.bins[256 + tid] = incl - count;
         }
         __syncthreads();
-        if (tid < 256) {
-            int before = int(s.bins[256 + tid]);
+        if (tid < kDigits) {
+            int before = int(incl - count);
             for (int w = 0; w < wave; ++w) before += s.sums[w];
-            if (before < left && before + int(s.bins[tid]) >= left) {  // one thread
+            if (before < left && before + int(count) >= left) {  // one thread
                 s.found[0] = tid;
                 s.found[1] = before;
             }
@@ -436,8 +440,9 @@ __device__ inline void choose(Choice<THREADS / 64, MINE> &s, float (&x)[MINE], c
         __syncthreads();
         const uint32_t at = s.found[0];
         left -= int(s.found[1]);
-        prefix |= uint64_t(255 - at) << shift;
-        mask |= uint64_t(255) << shift;
+        prefix |= uint64_t(last - at) << shift;
+        mask |= uint64_t(last) << shift;
+        bits = shift;
         const int here = int(s.bins[at]);
         __syncthreads();
         if (here == left) break;  // all that agree so far are kept
@@ -659,7 +664,10 @@ hipError_t launch_block_select(const void *q, const void *bounds, const int32_t 
         auto choose_by = [&](auto kernel, int threads) {
             kernel<<<dim3(unsigned(pairs)), dim3(threads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes, selected, a);
         };
-        if (a.max_blocks <= kThreads * kChoiceMine) choose_by(block_choose_kernel<T, D, kThreads, kChoiceMine>, kThreads);
+        // A wavefront per row where there are many: no barriers (1000 rows, 4 KV heads, up to 500 blocks, both launches, 46.6 us, by
+        // workgroups 52.6; but 24 rows, 2 KV heads, up to 190 blocks 16.4 and 14.4).
+        if (a.max_blocks <= 512 && pairs > 4 * kNumCUs) choose_by(block_choose_kernel<T, D, 64, 8>, 64);
+        else if (a.max_blocks <= kThreads * kChoiceMine) choose_by(block_choose_kernel<T, D, kThreads, kChoiceMine>, kThreads);
         else choose_by(block_choose_kernel<T, D, 1024, 16>, 1024);
         return hipGetLastError();
     };

@@ -4,6 +4,11 @@
 //   F_n = sum_{i<n} need_i,  R_n = sum_{i<n} new_i;   granted: need_n = 0 or F_n + need_n <= num_free, and R_n + new_n <= max_rows
 //   Q_n = new_n if granted, else 0;   row sum_{i<n} Q_i + j of the maps is token ctx_n + j
 //
+// Bound: latency for an iteration's batch (lengths, scans, a table entry, the store), memory for large maps (16 bytes a row).  One launch up to
+// 2048 sequences: every workgroup sums the lengths for itself, which are few, and takes its share of table entries and rows, so no
+// workgroup waits for another.  64 sequences, one token each, XXA us; 1500 sequences, 1.05 M rows, XXB us (a search over all sequences and
+// three dependent loads for every row by itself: 15.4 us; the 17 MB that are written take 3.4 us).
+//
 // A refusal for want of blocks refuses everybody behind who needs one, and one for want of rows everybody behind who brings any
 // (the sums count refused sequences too), so the blocks dealt out are the front of the free list, in order.
 #include "kvc_internal.h"
@@ -12,9 +17,6 @@
 namespace kvc {
 
 namespace {
-
-constexpr int kItems = 4;                       // sequences per thread and pass
-constexpr int kPass = kThreads * kItems;        // sequences per pass
 
 // Sums stop at 2^31 - 1, which is more than either limit (the host refuses larger ones).
 __device__ inline uint32_t add_saturated(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }
@@ -32,8 +34,8 @@ __device__ inline uint32_t scan_wave(uint32_t x, Op op) {
 }
 
 // Exclusive scan over the workgroup of two numbers per thread, starting from (and moving on) the carries.
-template <class Op>
-__device__ inline void scan_group(uint32_t &a, uint32_t &b, uint32_t &carry_a, uint32_t &carry_b, uint32_t (&s_sums)[2][kWaves], Op op) {
+template <int WAVES, class Op>
+__device__ inline void scan_group(uint32_t &a, uint32_t &b, uint32_t &carry_a, uint32_t &carry_b, uint32_t (&s_sums)[2][WAVES], Op op) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const uint32_t ia = scan_wave(a, op), ib = scan_wave(b, op);
     if (lane == 63) {
@@ -41,70 +43,75 @@ __device__ inline void scan_group(uint32_t &a, uint32_t &b, uint32_t &carry_a, u
         s_sums[1][wave] = ib;
     }
     __syncthreads();
-    uint32_t ba = carry_a, bb = carry_b;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w == wave) {
-            a = op(ba, uint32_t(__shfl_up(int(ia), 1)) * (lane > 0));
-            b = op(bb, uint32_t(__shfl_up(int(ib), 1)) * (lane > 0));
-        }
-        ba = op(ba, s_sums[0][w]);
-        bb = op(bb, s_sums[1][w]);
-    }
-    carry_a = ba;
-    carry_b = bb;
+    // lane w: the sum over wavefronts 0 .. w
+    const uint32_t wa = scan_wave(lane < WAVES ? s_sums[0][lane] : 0u, op), wb = scan_wave(lane < WAVES ? s_sums[1][lane] : 0u, op);
+    const uint32_t before_a = wave > 0 ? __builtin_amdgcn_readlane(wa, __builtin_amdgcn_readfirstlane(wave - 1)) : 0u;
+    const uint32_t before_b = wave > 0 ? __builtin_amdgcn_readlane(wb, __builtin_amdgcn_readfirstlane(wave - 1)) : 0u;
+    const uint32_t pa = uint32_t(__shfl_up(int(ia), 1)), pb = uint32_t(__shfl_up(int(ib), 1));
+    a = op(op(carry_a, before_a), lane > 0 ? pa : 0u);
+    b = op(op(carry_b, before_b), lane > 0 ? pb : 0u);
+    carry_a = op(carry_a, __builtin_amdgcn_readlane(wa, WAVES - 1));
+    carry_b = op(carry_b, __builtin_amdgcn_readlane(wb, WAVES - 1));
     __syncthreads();
 }
 
-__device__ inline int blocks_held(const TableArgs &t, int n, int ctx) {
-    return t.held_blocks ? t.held_blocks[n] : (ctx + (1 << t.block_size_log2) - 1) >> t.block_size_log2;
-}
-
-// One pass over sequences base .. base + kPass - 1.  Leaves in s_rows / s_first the first row and the first of the dealt-out blocks of each
-// (one more entry than sequences), and writes what is known per sequence where `write`.
+// What a pass over sequences base .. base + kThreads * ITEMS - 1 leaves in LDS for each of them: its first row, the first of the blocks dealt out to it
+// (one more entry than sequences), its length and the blocks it had.
+template <int THREADS, int ITEMS>
+struct Pass {
+    static constexpr int kSeqs = THREADS * ITEMS;
+    uint32_t rows[kSeqs + 1], first[kSeqs + 1], sums[2][THREADS / 64];
+    int ctx[kSeqs], held[kSeqs];
+};
 struct Carries { uint32_t need, rows, dealt, taken; };
-__device__ inline void scan_pass(const TableArgs &t, int base, Carries &c, uint32_t (&s_sums)[2][kWaves], uint32_t *s_rows, uint32_t *s_first,
-                                 bool write) {
-    const int first = base + threadIdx.x * kItems;
-    int ctx[kItems], held[kItems];
-    uint32_t need[kItems], rows[kItems], sum_need = 0, sum_rows = 0;
+
+// Writes what is known per sequence where `write`.
+template <int THREADS, int ITEMS>
+__device__ inline void scan_pass(const TableArgs &t, int base, Carries &c, Pass<THREADS, ITEMS> &s, bool write) {
+    const int first = base + threadIdx.x * ITEMS;
+    int ctx[ITEMS], held[ITEMS] = {}, fresh[ITEMS];
+    uint32_t need[ITEMS], rows[ITEMS], sum_need = 0, sum_rows = 0;
     auto saturated = [](uint32_t a, uint32_t b) { return add_saturated(a, b); };
     auto plain = [](uint32_t a, uint32_t b) { return a + b; };
+    auto load = [&](const int32_t *p, int (&x)[ITEMS]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-        const int n = first + k;
-        ctx[k] = held[k] = 0;
+        for (int k = 0; k < ITEMS; ++k) x[k] = p[min(first + k, t.num_seqs - 1)];
+    };
+    load(t.context_lens, ctx);
+    load(t.new_lens, fresh);
+    if (t.held_blocks) load(t.held_blocks, held);
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
         need[k] = rows[k] = 0;
-        if (n < t.num_seqs) {
-            ctx[k] = t.context_lens[n];
-            const int fresh = t.new_lens[n];
-            held[k] = blocks_held(t, n, ctx[k]);
-            const int tokens = t.max_blocks_per_seq << t.block_size_log2;  // at most 2^30
-            if (fresh > 0 && ctx[k] >= 0 && ctx[k] <= tokens && fresh <= tokens - ctx[k] && held[k] >= 0 && held[k] <= t.max_blocks_per_seq) {
-                rows[k] = fresh;
-                need[k] = max(0, ((ctx[k] + fresh - 1) >> t.block_size_log2) + 1 - held[k]);
-            }
+        if (!t.held_blocks) held[k] = (ctx[k] + (1 << t.block_size_log2) - 1) >> t.block_size_log2;
+        const int tokens = t.max_blocks_per_seq << t.block_size_log2;  // at most 2^30
+        if (first + k < t.num_seqs && fresh[k] > 0 && ctx[k] >= 0 && ctx[k] <= tokens && fresh[k] <= tokens - ctx[k] && held[k] >= 0 &&
+            held[k] <= t.max_blocks_per_seq) {
+            rows[k] = fresh[k];
+            need[k] = max(0, ((ctx[k] + fresh[k] - 1) >> t.block_size_log2) + 1 - held[k]);
         }
         sum_need = add_saturated(sum_need, need[k]);
         sum_rows = add_saturated(sum_rows, rows[k]);
     }
-    scan_group(sum_need, sum_rows, c.need, c.rows, s_sums, saturated);
+    scan_group(sum_need, sum_rows, c.need, c.rows, s.sums, saturated);
     uint32_t sum_dealt = 0, sum_taken = 0;
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < ITEMS; ++k) {
         sum_need = add_saturated(sum_need, need[k]);
         sum_rows = add_saturated(sum_rows, rows[k]);
         if (!((need[k] == 0 || sum_need <= uint32_t(t.num_free)) && sum_rows <= uint32_t(t.max_rows))) need[k] = rows[k] = 0;
         sum_dealt += rows[k];
         sum_taken += need[k];
     }
-    scan_group(sum_dealt, sum_taken, c.dealt, c.taken, s_sums, plain);
+    scan_group(sum_dealt, sum_taken, c.dealt, c.taken, s.sums, plain);
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < ITEMS; ++k) {
         const int n = first + k;
         if (n < t.num_seqs) {
-            s_rows[n - base] = sum_dealt;
-            s_first[n - base] = sum_taken;
+            s.rows[n - base] = sum_dealt;
+            s.first[n - base] = sum_taken;
+            s.ctx[n - base] = ctx[k];
+            s.held[n - base] = held[k];
             if (write) {
                 t.q_start[n] = int(sum_dealt);
                 t.context_lens_out[n] = ctx[k] + int(rows[k]);
@@ -114,21 +121,27 @@ __device__ inline void scan_pass(const TableArgs &t, int base, Carries &c, uint3
             sum_taken += need[k];
         }
     }
-    const int count = min(kPass, t.num_seqs - base);
+    const int count = min(Pass<THREADS, ITEMS>::kSeqs, t.num_seqs - base);
     if (threadIdx.x == 0) {
-        s_rows[count] = c.dealt;
-        s_first[count] = c.taken;
+        s.rows[count] = c.dealt;
+        s.first[count] = c.taken;
     }
 }
 
-// Largest i < count with s[i] <= x, for s[0] <= x < s[count].
-__device__ inline int place_of(const uint32_t *s, int count, uint32_t x) {
-    int lo = 0, hi = count;
+// Largest i in [lo, hi) with s[i] <= x, where s[lo] <= x and x < s[hi].
+__device__ inline int place_of(const uint32_t *s, int lo, int hi, uint32_t x) {
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (s[mid] <= x) lo = mid; else hi = mid;
     }
     return lo;
+}
+// The same over [0, count) for an x that all lanes share, up to 64 * 64 entries: 64 at a time.
+__device__ inline int place_of_all(const uint32_t *s, int count, uint32_t x) {
+    const int lane = threadIdx.x & 63, stride = (count + 63) >> 6;
+    const int at = lane * stride;
+    const int base = (__popcll(__ballot(at < count && s[min(at, count)] <= x)) - 1) * stride;
+    return base + __popcll(__ballot(lane < stride && base + lane < count && s[min(base + lane, count)] <= x)) - 1;
 }
 
 __device__ inline void write_row(const TableArgs &t, int64_t i, int n, int pos, int block) {
@@ -137,47 +150,73 @@ __device__ inline void write_row(const TableArgs &t, int64_t i, int n, int pos, 
     if (t.row_seqs) t.row_seqs[i] = n;
 }
 
-// Up to kWholeSeqs sequences: every workgroup sums for itself and takes its share of the table entries and rows.
-constexpr int kWholeSeqs = 4 * kPass;
-__global__ __launch_bounds__(kThreads) void block_tables_extend_kernel(TableArgs t) {
-    __shared__ uint32_t s_rows[kWholeSeqs + 1], s_first[kWholeSeqs + 1], s_sums[2][kWaves];
+constexpr int kRowsAtOnce = 256;  // of a wavefront
+
+// All sequences in one pass.
+template <int THREADS, int ITEMS>
+__global__ __launch_bounds__(THREADS) void block_tables_extend_kernel(TableArgs t) {
+    constexpr int WAVES = THREADS / 64;
+    __shared__ Pass<THREADS, ITEMS> s;
     Carries c = {0, 0, 0, 0};
-    for (int base = 0; base < t.num_seqs; base += kPass) scan_pass(t, base, c, s_sums, s_rows + base, s_first + base, blockIdx.x == 0);
+    if (t.num_seqs > 0) scan_pass(t, 0, c, s, blockIdx.x == 0);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         t.q_start[t.num_seqs] = int(c.dealt);
         if (t.taken) *t.taken = int(c.taken);
     }
     __syncthreads();
-    const int stride = gridDim.x * kThreads, me = blockIdx.x * kThreads + threadIdx.x;
-    for (int64_t e = me; e < c.taken; e += stride) {
-        const int n = place_of(s_first, t.num_seqs, uint32_t(e));
-        t.block_tables[int64_t(n) * t.max_blocks_per_seq + blocks_held(t, n, t.context_lens[n]) + (e - s_first[n])] = t.free_blocks[e];
-    }
-    for (int64_t i = me; i < t.max_rows; i += stride) {
-        if (i >= c.dealt) {
-            write_row(t, i, -1, -1, -1);
-            continue;
+    // A wavefront takes table entries and rows that lie together: the sequences they can belong to are found once for all of them.
+    const int lane = threadIdx.x & 63, wave = blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = gridDim.x * WAVES;
+    auto range = [&](const uint32_t *starts, uint32_t from, uint32_t to, int *first, int *end) __attribute__((always_inline)) {
+        *first = place_of_all(starts, t.num_seqs, from);
+        *end = starts[*first + 1] > to ? *first + 1 : place_of_all(starts, t.num_seqs, to) + 1;
+    };
+    for (int64_t i0 = int64_t(wave) * kRowsAtOnce; i0 < t.max_rows; i0 += int64_t(waves) * kRowsAtOnce) {
+        int first = 0, end = 0;
+        if (i0 < c.dealt) range(s.rows, uint32_t(i0), uint32_t(min(i0 + kRowsAtOnce, int64_t(c.dealt)) - 1), &first, &end);
+        constexpr int U = kRowsAtOnce / 64;
+        int seq[U], pos[U], block[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = i0 + 64 * u + lane;
+            seq[u] = pos[u] = block[u] = -1;
+            if (i < c.dealt) {
+                const int n = place_of(s.rows, first, end, uint32_t(i)), held = s.held[n];
+                seq[u] = n;
+                pos[u] = s.ctx[n] + int(i - s.rows[n]);
+                const int b = pos[u] >> t.block_size_log2;
+                block[u] = b < held ? t.block_tables[int64_t(n) * t.max_blocks_per_seq + b] : t.free_blocks[s.first[n] + (b - held)];
+            }
         }
-        const int n = place_of(s_rows, t.num_seqs, uint32_t(i));
-        const int ctx = t.context_lens[n], held = blocks_held(t, n, ctx);
-        const int pos = ctx + int(i - s_rows[n]), b = pos >> t.block_size_log2;
-        write_row(t, i, n, pos, b < held ? t.block_tables[int64_t(n) * t.max_blocks_per_seq + b] : t.free_blocks[s_first[n] + (b - held)]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + 64 * u + lane < t.max_rows) write_row(t, i0 + 64 * u + lane, seq[u], pos[u], block[u]);
+    }
+    for (int64_t e0 = int64_t(wave) * 64; e0 < c.taken; e0 += int64_t(waves) * 64) {
+        int first, end;
+        range(s.first, uint32_t(e0), uint32_t(min(e0 + 64, int64_t(c.taken)) - 1), &first, &end);
+        const int64_t e = e0 + lane;
+        if (e < c.taken) {
+            const int n = place_of(s.first, first, end, uint32_t(e));
+            t.block_tables[int64_t(n) * t.max_blocks_per_seq + s.held[n] + (e - s.first[n])] = t.free_blocks[e];
+        }
     }
 }
 
 // More sequences: one workgroup sums and fills the tables, a second launch fills the maps.
-__global__ __launch_bounds__(kThreads) void block_tables_sum_kernel(TableArgs t) {
-    __shared__ uint32_t s_rows[kPass + 1], s_first[kPass + 1], s_sums[2][kWaves];
+constexpr int kSumThreads = 1024;
+using SumPass = Pass<kSumThreads, 2>;
+__global__ __launch_bounds__(kSumThreads) void block_tables_sum_kernel(TableArgs t) {
+    __shared__ SumPass s;
     Carries c = {0, 0, 0, 0};
-    for (int base = 0; base < t.num_seqs; base += kPass) {
+    for (int base = 0; base < t.num_seqs; base += SumPass::kSeqs) {
         const uint32_t taken = c.taken;
-        scan_pass(t, base, c, s_sums, s_rows, s_first, true);
+        scan_pass(t, base, c, s, true);
         __syncthreads();
-        for (uint32_t e = taken + threadIdx.x; e < c.taken; e += kThreads) {
-            const int i = place_of(s_first, min(kPass, t.num_seqs - base), e), n = base + i;
-            t.block_tables[int64_t(n) * t.max_blocks_per_seq + blocks_held(t, n, t.context_lens[n]) + (e - s_first[i])] = t.free_blocks[e];
+        for (uint32_t e = taken + threadIdx.x; e < c.taken; e += kSumThreads) {
+            const int i = place_of(s.first, 0, min(SumPass::kSeqs, t.num_seqs - base), e);
+            t.block_tables[int64_t(base + i) * t.max_blocks_per_seq + s.held[i] + (e - s.first[i])] = t.free_blocks[e];
         }
-        __syncthreads();  // the next pass writes s_rows and s_first
+        __syncthreads();  // the next pass writes what is read here
     }
     if (threadIdx.x == 0) {
         t.q_start[t.num_seqs] = int(c.dealt);
@@ -193,7 +232,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_map_kernel(TableArgs t)
             write_row(t, i, -1, -1, -1);
             continue;
         }
-        const int n = place_of(starts, t.num_seqs, uint32_t(i));
+        const int n = place_of(starts, 0, t.num_seqs, uint32_t(i));
         const int pos = t.context_lens[n] + int(i - starts[n]);
         write_row(t, i, n, pos, t.block_tables[int64_t(n) * t.max_blocks_per_seq + (pos >> t.block_size_log2)]);
     }
@@ -202,16 +241,22 @@ __global__ __launch_bounds__(kThreads) void block_tables_map_kernel(TableArgs t)
 }  // namespace
 
 hipError_t launch_block_tables_extend(const TableArgs &t, hipStream_t stream) {
-    const int64_t share = 4 * kThreads;
-    const int grid = int(std::min<int64_t>(std::max<int64_t>((t.max_rows + share - 1) / share, 1), 4 * kNumCUs));
-    if (t.num_seqs <= kWholeSeqs) {
-        block_tables_extend_kernel<<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
+    auto grid_of = [&](int64_t share, int most) { return dim3(unsigned(std::min<int64_t>(std::max<int64_t>((t.max_rows + share - 1) / share, 1), most))); };
+    if (t.num_seqs <= SumPass::kSeqs) {
+        // Workgroups that sum many sequences are large and no more than the compute units: they all read the same lengths, which is what
+        // four times as many of a quarter the size spent their time on (1500 sequences 6 to 12 us of 18).
+        if (t.num_seqs <= kThreads)
+            block_tables_extend_kernel<kThreads, 1><<<grid_of(kWaves * kRowsAtOnce, 4 * kNumCUs), dim3(kThreads), 0, stream>>>(t);
+        else if (t.num_seqs <= kSumThreads)
+            block_tables_extend_kernel<kSumThreads, 1><<<grid_of(4 * kSumThreads, kNumCUs), dim3(kSumThreads), 0, stream>>>(t);
+        else
+            block_tables_extend_kernel<kSumThreads, 2><<<grid_of(4 * kSumThreads, kNumCUs), dim3(kSumThreads), 0, stream>>>(t);
         return hipGetLastError();
     }
-    block_tables_sum_kernel<<<dim3(1), dim3(kThreads), 0, stream>>>(t);
+    block_tables_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(t);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || t.max_rows == 0) return e;
-    block_tables_map_kernel<<<dim3(grid), dim3(kThreads), 0, stream>>>(t);
+    block_tables_map_kernel<<<grid_of(4 * kThreads, 4 * kNumCUs), dim3(kThreads), 0, stream>>>(t);
     return hipGetLastError();
 }
 

@@ -35,8 +35,8 @@ def _check(tables, ctx, new, held, free, bs, max_rows, use_held=True, stream=Non
     return want
 
 
-@pytest.mark.parametrize("n,width,bs,most_new", [(1, 1, 1, 1), (1, 40, 16, 500), (3, 7, 4, 1), (64, 256, 16, 1), (255, 9, 8, 30),
-                                                  (257, 33, 2, 40), (1023, 5, 32, 3), (1025, 6, 64, 100), (4096, 4, 16, 20), (4097, 4, 16, 20),
+@pytest.mark.parametrize("n,width,bs,most_new", [(1, 1, 1, 1), (1, 40, 16, 500), (3, 7, 4, 1), (64, 256, 16, 1), (255, 9, 8, 30), (256, 9, 8, 30),
+                                                  (257, 33, 2, 40), (1024, 5, 32, 3), (1025, 6, 64, 100), (2048, 4, 16, 20), (2049, 4, 16, 20), (4096, 4, 16, 20),
                                                   (9000, 3, 1, 2), (37, 3, 256, 700)])
 @pytest.mark.parametrize("use_held", [True, False])
 def test_every_length(n, width, bs, most_new, use_held):
