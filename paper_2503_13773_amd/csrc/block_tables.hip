@@ -150,12 +150,10 @@ __device__ inline void write_row(const TableArgs &t, int64_t i, int n, int pos, 
     if (t.row_seqs) t.row_seqs[i] = n;
 }
 
-constexpr int kRowsAtOnce = 256;  // of a wavefront
-
-// All sequences in one pass.
-template <int THREADS, int ITEMS>
+// All sequences in one pass.  A wavefront takes 64 * U rows at a time.
+template <int THREADS, int ITEMS, int U>
 __global__ __launch_bounds__(THREADS) void block_tables_extend_kernel(TableArgs t) {
-    constexpr int WAVES = THREADS / 64;
+    constexpr int WAVES = THREADS / 64, kRowsAtOnce = 64 * U;
     __shared__ Pass<THREADS, ITEMS> s;
     Carries c = {0, 0, 0, 0};
     if (t.num_seqs > 0) scan_pass(t, 0, c, s, blockIdx.x == 0);
@@ -173,14 +171,22 @@ __global__ __launch_bounds__(THREADS) void block_tables_extend_kernel(TableArgs 
     for (int64_t i0 = int64_t(wave) * kRowsAtOnce; i0 < t.max_rows; i0 += int64_t(waves) * kRowsAtOnce) {
         int first = 0, end = 0;
         if (i0 < c.dealt) range(s.rows, uint32_t(i0), uint32_t(min(i0 + kRowsAtOnce, int64_t(c.dealt)) - 1), &first, &end);
-        constexpr int U = kRowsAtOnce / 64;
-        int seq[U], pos[U], block[U];
+        int n_of[U], seq[U], pos[U], block[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) n_of[u] = first;
+        for (int left = end - first; left > 1;) {  // the largest with rows[n] <= i, for all U rows of a lane at once
+            const int half = left >> 1;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (s.rows[n_of[u] + half] <= uint32_t(i0) + 64 * u + lane) n_of[u] += half;
+            left -= half;
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t i = i0 + 64 * u + lane;
             seq[u] = pos[u] = block[u] = -1;
             if (i < c.dealt) {
-                const int n = place_of(s.rows, first, end, uint32_t(i)), held = s.held[n];
+                const int n = n_of[u], held = s.held[n];
                 seq[u] = n;
                 pos[u] = s.ctx[n] + int(i - s.rows[n]);
                 const int b = pos[u] >> t.block_size_log2;
@@ -245,12 +251,18 @@ hipError_t launch_block_tables_extend(const TableArgs &t, hipStream_t stream) {
     if (t.num_seqs <= SumPass::kSeqs) {
         // Workgroups that sum many sequences are large and no more than the compute units: they all read the same lengths, which is what
         // four times as many of a quarter the size spent their time on (1500 sequences 6 to 12 us of 18).
-        if (t.num_seqs <= kThreads)
-            block_tables_extend_kernel<kThreads, 1><<<grid_of(kWaves * kRowsAtOnce, 4 * kNumCUs), dim3(kThreads), 0, stream>>>(t);
-        else if (t.num_seqs <= kSumThreads)
-            block_tables_extend_kernel<kSumThreads, 1><<<grid_of(4 * kSumThreads, kNumCUs), dim3(kSumThreads), 0, stream>>>(t);
-        else
-            block_tables_extend_kernel<kSumThreads, 2><<<grid_of(4 * kSumThreads, kNumCUs), dim3(kSumThreads), 0, stream>>>(t);
+        // A wavefront takes 64 rows where the workgroups of the launch have enough of them, else 256 at a time.
+#define KVC_EXTEND(THREADS, ITEMS, GROUPS)                                                                                              \
+    do {                                                                                                                                \
+        if (t.max_rows <= int64_t(GROUPS) * THREADS / 4)                                                                                \
+            block_tables_extend_kernel<THREADS, ITEMS, 1><<<grid_of(THREADS, GROUPS), dim3(THREADS), 0, stream>>>(t);                   \
+        else                                                                                                                            \
+            block_tables_extend_kernel<THREADS, ITEMS, 4><<<grid_of(4 * THREADS, GROUPS), dim3(THREADS), 0, stream>>>(t);               \
+    } while (0)
+        if (t.num_seqs <= kThreads) KVC_EXTEND(kThreads, 1, 4 * kNumCUs);
+        else if (t.num_seqs <= kSumThreads) KVC_EXTEND(kSumThreads, 1, kNumCUs);
+        else KVC_EXTEND(kSumThreads, 2, kNumCUs);
+#undef KVC_EXTEND
         return hipGetLastError();
     }
     block_tables_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(t);
