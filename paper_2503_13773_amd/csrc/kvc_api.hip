@@ -316,14 +316,14 @@ int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, 
         a.units_per_block_log2 = a.block_size_log2 - a.unit_log2;
         a.tiles = int(ceil_div(int64_t(budget) << a.block_size_log2, 32));
         a.wave_per_unit = units >= kSelectedManyUnits;
-        a.waves = units <= kSelectedFewUnits ? 8 : 4;
+        a.waves = units <= kSelectedFewUnits || (units > kvc::kNumCUs / 2 && units <= kvc::kNumCUs) ? 8 : 4;
         trip = a.waves;
     } else {
         a.tiles = budget;
         trip = std::max(1, 64 >> a.block_size_log2);
     }
     const int64_t most = std::min<int64_t>(kvc::kMaxSelectedParts, ceil_div(a.tiles, trip));
-    const int64_t parts = units > 0 ? std::max<int64_t>(1, std::min<int64_t>(kSelectedGroups / units, most)) : 1;
+    const int64_t parts = units > 0 ? std::max<int64_t>(1, std::min<int64_t>((units > kvc::kNumCUs / 2 && a.on_mfma ? kvc::kNumCUs : kSelectedGroups) / units, most)) : 1;
     a.tiles_per_part = int(ceil_div(a.tiles, parts));
     a.parts = int(ceil_div(a.tiles, a.tiles_per_part));
     pl->ml_offset = pl->bytes = 0;

@@ -477,6 +477,20 @@ __device__ inline float sum_over_lanes(float x) {
     }
     return x;
 }
+// op over the lanes that hold the same dims of the wavefront's tokens, LR apart.
+template <int LR, class Op>
+__device__ inline float over_tokens(float x, Op op) {
+    if constexpr (LR <= 8) x = op(x, lanes::permuted<lanes::kRor8>(x));
+    if constexpr (LR <= 16) {
+        const lanes::Pair<float> a = lanes::pair_of<16>(x);
+        x = op(a.first, a.second);
+    }
+    const lanes::Pair<float> b = lanes::pair_of<32>(x);
+    return op(b.first, b.second);
+}
+// exp(d) for d <= 0, as a power of two: the rounding of the product moves a weight by 2^-24 of its own exponent, 3e-8 of the largest weight
+// at most.  An expf is fifteen instructions, and the lanes of a token all compute the same one.
+__device__ inline float weight_of(float d) { return __builtin_amdgcn_exp2f(d * 1.44269504088896340736f); }
 __device__ inline void store_device(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ inline float load_device(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
@@ -519,8 +533,9 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
         int last = 0;
         for (int i = tid; i < min(kWindow, end - e0); i += kThreads) {
             const int b = list[e0 + i];
+            const int named = table[min(max(b, 0), a.max_blocks_per_seq - 1)];  // without waiting for the position
             const bool there = b >= 0 && b <= own;
-            s_entry[i] = int2{there ? table[b] : own_block, there ? min(u.pos + 1 - (b << bs_log2), 1 << bs_log2) : 0};
+            s_entry[i] = int2{there ? named : own_block, there ? min(u.pos + 1 - (b << bs_log2), 1 << bs_log2) : 0};
             if (there) last = i + 1;
         }
         if (last > 0) atomicMax(&s_last, last);
@@ -555,14 +570,14 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
                     s[i] = counts[i] ? sum_over_lanes<LR>(d) * a.scale : -INFINITY;
                     top = fmaxf(top, s[i]);
                 }
-                const float alpha = expf(m[h] - top);
+                const float alpha = weight_of(m[h] - top);
                 m[h] = top;
                 l[h] *= alpha;
 #pragma unroll
                 for (int j = 0; j < N; ++j) acc[h][j] *= alpha;
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    const float p = expf(s[i] - top);
+                    const float p = weight_of(s[i] - top);
                     l[h] += p;
 #pragma unroll
                     for (int j = 0; j < N; ++j) acc[h][j] = fmaf(p, vf[i][j], acc[h][j]);
@@ -573,14 +588,12 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
     }
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {  // the lane groups of the wavefront
+        const float top = over_tokens<LR>(m[h], [](float u, float v) { return fmaxf(u, v); }), mine = weight_of(m[h] - top);
+        auto add = [](float u, float v) { return u + v; };
+        l[h] = over_tokens<LR>(l[h] * mine, add);
 #pragma unroll
-        for (int off = LR; off < 64; off <<= 1) {
-            const float other = __shfl_xor(m[h], off), top = fmaxf(m[h], other), mine = expf(m[h] - top), theirs = expf(other - top);
-            l[h] = l[h] * mine + __shfl_xor(l[h], off) * theirs;
-#pragma unroll
-            for (int i = 0; i < N; ++i) acc[h][i] = acc[h][i] * mine + __shfl_xor(acc[h][i], off) * theirs;
-            m[h] = top;
-        }
+        for (int i = 0; i < N; ++i) acc[h][i] = over_tokens<LR>(acc[h][i] * mine, add);
+        m[h] = top;
         if (tg == 0) {
 #pragma unroll
             for (int i = 0; i < N; ++i) s_acc[wave][h][c * N + i] = acc[h][i];
@@ -597,7 +610,7 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
         float M = -FLT_MAX, L = 0.f, A = 0.f;
         for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][h]);
         for (int w = 0; w < kWaves; ++w) {
-            const float wgt = expf(s_m[w][h] - M);
+            const float wgt = weight_of(s_m[w][h] - M);
             L = fmaf(wgt, s_l[w][h], L);
             A = fmaf(wgt, s_acc[w][h][d], A);
         }
@@ -637,7 +650,7 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
                 if (p0 + j >= parts) break;
-                const float wgt = s_m[p0 + j][h] == -INFINITY ? 0.f : expf(s_m[p0 + j][h] - M);
+                const float wgt = s_m[p0 + j][h] == -INFINITY ? 0.f : weight_of(s_m[p0 + j][h] - M);
                 L = fmaf(wgt, s_l[p0 + j][h], L);
                 A = fmaf(wgt, y[j], A);
             }
