@@ -286,9 +286,15 @@ struct SelectedPlan {
     kvc::SelectedArgs a;
     uint64_t ml_offset, bytes;  // of the workspace: counters, then the parts' accumulators, then their maxima and sums
 };
-constexpr int kSelectedGroups = 512;  // workgroups that few units are cut into
-constexpr int kSelectedFewUnits = 32;     // up to here workgroups of eight wavefronts
-constexpr int kSelectedManyUnits = 2048;  // from here on a wavefront takes a unit
+// Units of up to half a compute unit each are cut into kSelectedGroups workgroups in all, more are not cut: 256 units of 32 long documents, 64 / 8
+// heads of 128, 43.3 us whole with eight wavefronts, in two parts each 47.5 (but 96 of up to 512 tokens 9.3 in parts, whole 10.7).  Eight wavefronts
+// up to kSelectedFewUnits and for the 256: one document 9.1 us, with four 9.6; 64 units 17.5 with four, with eight 21.5.
+constexpr int kSelectedGroups = 512;
+constexpr int kSelectedFewUnits = 32;
+// Rows of chunks: from here on a wavefront takes a unit (1000 rows, 32 / 8 heads of 64: 93 us, by workgroups 171; 200 rows, 32 / 8 heads of 128
+// 19.8 and 25.7; but 136 rows 18.8 and 19.6, 240 rows of heads of 64 33.5 and 31.7).  Not in a decode step, whose units share nothing (150
+// requests, 134 and 115 us).
+constexpr int kSelectedManyUnits = 1024;
 int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, SelectedPlan *pl) {
     const int rc = check_rows(d, total_q);
     if (rc != KVC_OK) return rc;
@@ -315,15 +321,21 @@ int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, 
         a.unit_log2 = std::min(a.block_size_log2, 5);  // a tile is 32 tokens
         a.units_per_block_log2 = a.block_size_log2 - a.unit_log2;
         a.tiles = int(ceil_div(int64_t(budget) << a.block_size_log2, 32));
-        a.wave_per_unit = units >= kSelectedManyUnits;
+        a.wave_per_unit = total_q > d->num_seqs && units >= kSelectedManyUnits;
         a.waves = units <= kSelectedFewUnits || (units > kvc::kNumCUs / 2 && units <= kvc::kNumCUs) ? 8 : 4;
         trip = a.waves;
     } else {
         a.tiles = budget;
-        trip = std::max(1, 64 >> a.block_size_log2);
+        // Tokens that four wavefronts take at once, 4 KiB of K each.  Sixteen where they all fit the device, have more than two such trips to
+        // make (fp32, 16 / 4 heads, 33 lists of 256 tokens of 128, us with four / sixteen: 17.3 / 12.3, one of 1024 tokens of 64 13.1 / 10.7; 45
+        // of 128 of 64, two trips, 6.3 / 7.5), and the registers allow it (four heads in bf16 spill).
+        const int tokens = 4 * 4096 / (d->head_dim * (d->dtype == KVC_F32 ? 4 : 2));
+        const bool wide = units <= kvc::kNumCUs && (int64_t(budget) << a.block_size_log2) > 2 * tokens && (d->dtype == KVC_F32 || heads < 4);
+        a.waves = wide ? 16 : 4;
+        trip = std::max(1, (tokens * a.waves / 4) >> a.block_size_log2);
     }
     const int64_t most = std::min<int64_t>(kvc::kMaxSelectedParts, ceil_div(a.tiles, trip));
-    const int64_t parts = units > 0 ? std::max<int64_t>(1, std::min<int64_t>((units > kvc::kNumCUs / 2 && a.on_mfma ? kvc::kNumCUs : kSelectedGroups) / units, most)) : 1;
+    const int64_t parts = units > 0 ? std::max<int64_t>(1, std::min<int64_t>((units > kvc::kNumCUs / 2 || !a.on_mfma ? kvc::kNumCUs : kSelectedGroups) / units, most)) : 1;
     a.tiles_per_part = int(ceil_div(a.tiles, parts));
     a.parts = int(ceil_div(a.tiles, a.tiles_per_part));
     pl->ml_offset = pl->bytes = 0;

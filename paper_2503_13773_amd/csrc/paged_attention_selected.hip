@@ -495,15 +495,15 @@ __device__ inline void store_device(float *p, float x) { __hip_atomic_store(p, x
 __device__ inline float load_device(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // Grid as above, the chunk of heads HEADS of them.
-template <class T, int D, int HEADS>
-__global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__restrict__ q, const T *__restrict__ k_cache, const T *__restrict__ v_cache,
+template <class T, int D, int HEADS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void pa_selected_valu_kernel(const T *__restrict__ q, const T *__restrict__ k_cache, const T *__restrict__ v_cache,
                                                                     const int32_t *__restrict__ block_tables, const int32_t *__restrict__ context_lens,
                                                                     const int32_t *__restrict__ q_start, const int32_t *__restrict__ selected,
                                                                     T *__restrict__ out, Workspace ws, SelectedArgs a) {
     constexpr int N = Vec<T>::N, LR = D / N, TOKENS = 64 / LR, U = 4;
     __shared__ int2 s_entry[kWindow];  // pool index of a block, tokens of it that count
     __shared__ int s_last;
-    __shared__ float s_m[kMaxSelectedParts][HEADS], s_l[kMaxSelectedParts][HEADS], s_acc[kWaves][HEADS][D];  // of the wavefronts; m, l of the parts
+    __shared__ float s_m[kMaxSelectedParts][HEADS], s_l[kMaxSelectedParts][HEADS], s_acc[WAVES][HEADS][D];  // of the wavefronts; m, l of the parts
     const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, c = lane % LR, tg = lane / LR;
     const int row = blockIdx.x / a.num_kv_heads, parts = a.parts, part = blockIdx.z;
     const Unit u(a, q_start, context_lens, row, blockIdx.x - row * a.num_kv_heads, blockIdx.y);
@@ -511,7 +511,7 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
     T *dst = out + (int64_t(row) * a.num_q_heads + u.head0) * D;
     if (u.pos < 0) {
         if (part == 0)
-            for (int i = tid; i < HEADS * D; i += kThreads) dst[i] = T(0);
+            for (int i = tid; i < HEADS * D; i += (64 * WAVES)) dst[i] = T(0);
         return;
     }
     float x[HEADS][N], m[HEADS], l[HEADS], acc[HEADS][N];
@@ -531,7 +531,7 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
         if (tid == 0) s_last = 0;
         __syncthreads();
         int last = 0;
-        for (int i = tid; i < min(kWindow, end - e0); i += kThreads) {
+        for (int i = tid; i < min(kWindow, end - e0); i += (64 * WAVES)) {
             const int b = list[e0 + i];
             const int named = table[min(max(b, 0), a.max_blocks_per_seq - 1)];  // without waiting for the position
             const bool there = b >= 0 && b <= own;
@@ -542,7 +542,7 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
         __syncthreads();
         const int tokens = s_last << bs_log2;
         any |= tokens > 0;
-        for (int t0 = wave * TOKENS * U; t0 < tokens; t0 += kWaves * TOKENS * U) {
+        for (int t0 = wave * TOKENS * U; t0 < tokens; t0 += WAVES * TOKENS * U) {
             float kf[U][N], vf[U][N];
             bool counts[U];
 #pragma unroll
@@ -605,11 +605,11 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
     }
     __syncthreads();
     const int64_t unit = int64_t(blockIdx.x) * gridDim.y + blockIdx.y, slot0 = unit * parts;
-    for (int f = tid; f < HEADS * D; f += kThreads) {
+    for (int f = tid; f < HEADS * D; f += (64 * WAVES)) {
         const int h = f / D, d = f % D;
         float M = -FLT_MAX, L = 0.f, A = 0.f;
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][h]);
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) M = fmaxf(M, s_m[w][h]);
+        for (int w = 0; w < WAVES; ++w) {
             const float wgt = weight_of(s_m[w][h] - M);
             L = fmaf(wgt, s_l[w][h], L);
             A = fmaf(wgt, s_acc[w][h][d], A);
@@ -633,12 +633,12 @@ __global__ __launch_bounds__(kThreads) void pa_selected_valu_kernel(const T *__r
     if (!s_last) return;
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
     if (tid == 0) __hip_atomic_store(ws.cnt + unit * a.counter_step, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int i = tid; i < parts * HEADS; i += kThreads) {
+    for (int i = tid; i < parts * HEADS; i += (64 * WAVES)) {
         s_m[i / HEADS][i % HEADS] = load_device(ws.ml + (slot0 * HEADS + i) * 2);
         s_l[i / HEADS][i % HEADS] = load_device(ws.ml + (slot0 * HEADS + i) * 2 + 1);
     }
     __syncthreads();
-    for (int f = tid; f < HEADS * D; f += kThreads) {
+    for (int f = tid; f < HEADS * D; f += (64 * WAVES)) {
         const int h = f / D;
         float M = -INFINITY, L = 0.f, A = 0.f;
         for (int p = 0; p < parts; ++p) M = fmaxf(M, s_m[p][h]);
@@ -692,14 +692,19 @@ hipError_t launch_attention_selected(const void *q, const void *k_cache, const v
     }
     auto launch = [&](auto kernel, auto type) {
         using T = decltype(type);
-        kernel<<<grid, dim3(kThreads), 0, stream>>>(static_cast<const T *>(q), static_cast<const T *>(k_cache), static_cast<const T *>(v_cache), block_tables,
+        kernel<<<grid, dim3(64 * a.waves), 0, stream>>>(static_cast<const T *>(q), static_cast<const T *>(k_cache), static_cast<const T *>(v_cache), block_tables,
                                                     context_lens, q_start, selected, static_cast<T *>(out), ws, a);
     };
-#define KVC_SELECTED(T, D)                                                          \
-    do {                                                                            \
-        if (a.heads_per_chunk == 4) launch(pa_selected_valu_kernel<T, D, 4>, T());  \
-        else if (a.heads_per_chunk == 2) launch(pa_selected_valu_kernel<T, D, 2>, T()); \
-        else launch(pa_selected_valu_kernel<T, D, 1>, T());                         \
+#define KVC_SELECTED_WAVES(T, D, HEADS)                                                       \
+    do {                                                                                      \
+        if (a.waves == 16) launch(pa_selected_valu_kernel<T, D, HEADS, 16>, T());             \
+        else launch(pa_selected_valu_kernel<T, D, HEADS, 4>, T());                            \
+    } while (0)
+#define KVC_SELECTED(T, D)                                                                    \
+    do {                                                                                      \
+        if (a.heads_per_chunk == 4) KVC_SELECTED_WAVES(T, D, 4);                              \
+        else if (a.heads_per_chunk == 2) KVC_SELECTED_WAVES(T, D, 2);                         \
+        else KVC_SELECTED_WAVES(T, D, 1);                                                     \
     } while (0)
     if (dtype == KVC_F32) {
         if (head_dim == 64) KVC_SELECTED(float, 64); else KVC_SELECTED(float, 128);
@@ -707,6 +712,7 @@ hipError_t launch_attention_selected(const void *q, const void *k_cache, const v
         if (head_dim == 64) KVC_SELECTED(uint16_t, 64); else KVC_SELECTED(uint16_t, 128);
     }
 #undef KVC_SELECTED
+#undef KVC_SELECTED_WAVES
     return hipGetLastError();
 }
 
