@@ -6,9 +6,13 @@ paper Sections 3.3-3.5); this module only keeps the books the decisions refer to
 owns which blocks, who is embedded where, what sits in the swap space) and turns them into the
 device calls of include/kvc.h:
 
-    kv_cache_append            the new token of every batched request, and the K/V of a request
-                               that is admitted or recomputed
-    paged_attention_decode     one decode iteration over the batch
+    kv_cache_append            the new token of every batched request
+    block_tables_extend and    the slots of all tokens of a request that is admitted or recomputed, and
+    kv_cache_write             their K/V in one call
+    paged_attention_decode     one decode iteration over the batch; with ``sparse_budget`` its place is taken by
+    key_bounds_update,         the bounds of the blocks that new tokens filled, the blocks that each query
+    block_select and           keeps, and attention over these
+    paged_attention_selected
     paged_attention_prefill    the attention of an admitted or recomputed request over all its
                                positions (the recomputation path)
     kv_block_copy              swap-out to / swap-in from pinned host memory
@@ -57,7 +61,9 @@ class ServedRequest:
 class HipOps:
     """The device side: pools in HBM, swap space in pinned host memory, calls through the C ABI."""
 
-    def __init__(self, num_blocks: int, swap_blocks: int, hq: int, hkv: int, d: int, block_size: int):
+    def __init__(self, num_blocks: int, swap_blocks: int, hq: int, hkv: int, d: int, block_size: int,
+                 sparse_budget: Optional[int] = None):
+        """sparse_budget: blocks that a decode query attends to at most (the first one, the last two, the best of the others)."""
         import torch
 
         from . import binding as K
@@ -65,6 +71,8 @@ class HipOps:
         self.pool = torch.zeros((2, num_blocks, hkv, block_size, d), dtype=torch.bfloat16, device="cuda")
         self.swap = torch.zeros((2, max(1, swap_blocks), hkv, block_size, d), dtype=torch.bfloat16, pin_memory=True)
         self.scale = 1.0 / math.sqrt(d)
+        self.block_size, self.sparse_budget = block_size, sparse_budget
+        self.bounds = K.new_key_bounds(self.pool[0]) if sparse_budget else None
 
     def _bf16(self, a: np.ndarray):
         return self.torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).cuda().view(self.torch.bfloat16)
@@ -73,10 +81,29 @@ class HipOps:
         return self.torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
 
     def append(self, k_new, v_new, tables, positions) -> None:
+        tables = self._i32(tables)
         self.K.kv_cache_append(self._bf16(k_new), self._bf16(v_new), self.pool[0], self.pool[1],
-                               self._i32(tables), self._i32(positions))
+                               tables, self._i32(positions))
+        if self.sparse_budget:
+            self.K.key_bounds_update(self.pool[0], self.bounds, tables, self._i32(np.asarray(positions) + 1))
+
+    def append_rows(self, k_new, v_new, tables, held_blocks) -> None:
+        """K/V of the first len(k_new) positions of one request, whose table row names `held_blocks` blocks."""
+        n, tables = len(k_new), self._i32(tables)
+        none = self._i32(np.zeros(0))
+        u = self.K.block_tables_extend(tables, self._i32([0]), self._i32([n]), none, self.block_size, max_rows=n,
+                                       held_blocks=self._i32([held_blocks]))
+        self.K.kv_cache_write(self._bf16(k_new), self._bf16(v_new), self.pool[0], self.pool[1], u.slot_map)
+        if self.sparse_budget:
+            self.K.key_bounds_update(self.pool[0], self.bounds, tables, u.context_lens, u.q_start, n)
 
     def decode(self, q, tables, lens) -> np.ndarray:
+        if self.sparse_budget:
+            q, tables, lens = self._bf16(q), self._i32(tables), self._i32(lens)
+            kept = self.K.block_select(q, self.bounds, tables, lens, self.sparse_budget, block_size=self.block_size,
+                                       keep_first=min(1, self.sparse_budget - 1), keep_last=min(2, self.sparse_budget))
+            out = self.K.paged_attention_selected(q, self.pool[0], self.pool[1], tables, lens, kept, self.scale)
+            return out.float().cpu().numpy()
         out = self.K.paged_attention_decode(self._bf16(q), self.pool[0], self.pool[1], self._i32(tables),
                                             self._i32(lens), self.scale)
         return out.float().cpu().numpy()
@@ -95,6 +122,9 @@ class HipOps:
     def copy_in(self, slots, block_ids) -> None:
         m = self.torch.tensor(list(zip(slots, block_ids)), dtype=self.torch.int64).cuda()
         self.K.kv_block_copy(self.swap, self.pool, m)
+        if self.sparse_budget and block_ids:   # all their tokens are new to these blocks
+            n = len(block_ids) * self.block_size
+            self.K.key_bounds_update(self.pool[0], self.bounds, self._i32([block_ids]), self._i32([n]), self._i32([0, n]), n)
 
     def poison(self, block_ids) -> None:
         """Released blocks hold garbage from now on (NaN here, so that a stale reference shows)."""
@@ -265,9 +295,12 @@ class KvcServer:
                 n_tok = r.prompt_len if r.state == NEW else r.length
                 table = np.full((1, self.lmax), -1, dtype=np.int32)
                 table[0, :len(r.blocks)] = r.blocks
-                for pos in range(n_tok):              # K/V of every position, as the model would produce them
-                    k, v = self.kv_fn(r.rid, pos)
-                    self.ops.append(k[None], v[None], table, np.array([pos], dtype=np.int32))
+                kv = [self.kv_fn(r.rid, pos) for pos in range(n_tok)]   # as the model would produce them
+                if hasattr(self.ops, "append_rows"):
+                    self.ops.append_rows(np.stack([k for k, _ in kv]), np.stack([v for _, v in kv]), table, len(r.blocks))
+                else:
+                    for pos, (k, v) in enumerate(kv):
+                        self.ops.append(k[None], v[None], table, np.array([pos], dtype=np.int32))
                 q = np.stack([self.q_fn(r.rid, pos) for pos in range(n_tok)])
                 result["prefill"][r.rid] = self.ops.prefill(q, table, np.array([n_tok], dtype=np.int32),
                                                             np.array([0, n_tok], dtype=np.int32))
