@@ -62,13 +62,17 @@ struct Load<uint16_t> {
 
 // ---- scores from the matrix cores
 
-// An operand: 8 numbers of a lane.  bf16 as they are; fp32 as the sum of two bf16 values (2^-17 relative).
+// An operand: 8 numbers of a lane.  bf16 as they are (the matrix cores keep subnormal numbers); fp32 as the sum of two bf16 values, 2^-17 relative
+// or, below the normal numbers, 2^-134.  Bounds smaller than kSmallest count as that in the sum of sizes, whose share of slack (over 2^-14 of
+// it) is more than they can lose; queries with numbers below 2^-100 are left to 64 bits.
+constexpr float kSmallest = 0x1p-118f;
 template <class T>
 struct Operand;
 template <>
 struct Operand<uint16_t> {
     uint4 w;
     __device__ void load(const uint16_t *p) { w = *reinterpret_cast<const uint4 *>(p); }
+    __device__ bool too_small() const { return false; }
     __device__ static uint32_t negative(uint32_t x) { return ((x >> 15) & 0x10001u) * 0xffffu; }
     __device__ Operand plus() const { return {uint4{w.x & ~negative(w.x), w.y & ~negative(w.y), w.z & ~negative(w.z), w.w & ~negative(w.w)}}; }
     __device__ Operand minus() const { return {uint4{w.x & negative(w.x), w.y & negative(w.y), w.z & negative(w.z), w.w & negative(w.w)}}; }
@@ -93,6 +97,12 @@ struct Operand<float> {
         const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
         x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
         x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+    __device__ bool too_small() const {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) any |= x[i] != 0.f && fabsf(x[i]) < 0x1p-100f;
+        return any;
     }
     __device__ void split() {
         uint32_t h[4], l[4];
@@ -122,7 +132,7 @@ struct Operand<float> {
         uint32_t s[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            s[i] = pack_bf16(fmaxf(fabsf(a.x[2 * i]), fabsf(b.x[2 * i])), fmaxf(fabsf(a.x[2 * i + 1]), fabsf(b.x[2 * i + 1])));
+            s[i] = pack_bf16(fmaxf(fmaxf(fabsf(a.x[2 * i]), fabsf(b.x[2 * i])), kSmallest), fmaxf(fmaxf(fabsf(a.x[2 * i + 1]), fabsf(b.x[2 * i + 1])), kSmallest));
         return __builtin_bit_cast(bf16x8, uint4{s[0], s[1], s[2], s[3]});
     }
     __device__ bf16x8 top() const { return hi; }
@@ -196,7 +206,6 @@ struct Exactly {
     }
 };
 
-constexpr int kChoiceMine = 8;  // scores that a thread holds where a workgroup of kThreads chooses
 
 // What a workgroup shares while it chooses.
 template <int WAVES, int MINE>
@@ -460,17 +469,21 @@ __device__ inline void choose(Choice<THREADS / 64, MINE> &s, float (&x)[MINE], c
 // times 16 / heads rows; GROUPS such sets of rows share the loads.  Rows of products are 16 blocks.  blockIdx.x = KV head + KV heads * tile of
 // rows (tile_rows: one of a decode step, as many as there are columns for of chunks), blockIdx.y = share of the blocks.  Writes the scores of all
 // rows of the tile, and per row and share the largest sum of sizes.
-// HERE (tiles of one row): the workgroup that finishes a row and KV head's last share chooses for it.  Scores and sizes travel by device-scope
-// accesses; each workgroup waits for its own and counts itself; nobody waits for anybody.
-template <class T, int D, int GROUPS, bool HERE>
-__global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restrict__ q, const T *__restrict__ bounds, const int32_t *__restrict__ block_tables,
+// MINE > 0 (tiles of one row): the workgroup that finishes a row and KV head's last share chooses for it, MINE blocks a thread at most.  Scores and
+// sizes travel by device-scope accesses; each workgroup waits for its own and counts itself; nobody waits for anybody.  A single share's
+// scores stay in LDS.
+template <class T, int D, int GROUPS, int THREADS, int MINE>
+__global__ __launch_bounds__(THREADS) void block_scores_kernel(const T *__restrict__ q, const T *__restrict__ bounds, const int32_t *__restrict__ block_tables,
                                                                 const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start,
                                                                 float *__restrict__ scores, float *__restrict__ sizes, int32_t *__restrict__ counters,
                                                                 int32_t *__restrict__ selected, SelectArgs a, int tile_rows) {
-    constexpr int J = D / 32;
+    constexpr int J = D / 32, WAVES = THREADS / 64;
+    constexpr bool HERE = MINE > 0;
     using Op = Operand<T>;
-    __shared__ float s_size[kWaves][GROUPS][16];
-    __shared__ std::conditional_t<HERE, Choice<kWaves, kChoiceMine>, int> s_choice;
+    __shared__ float s_size[WAVES][GROUPS][16];
+    __shared__ std::conditional_t<HERE, Choice<WAVES, HERE ? MINE : 1>, int> s_choice;
+    __shared__ float s_scores[HERE ? THREADS * MINE : 1];
+    __shared__ float s_whole_size;
     __shared__ int s_last;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, quad = lane >> 4, r = lane & 15;
     const int tile = blockIdx.x / a.num_kv_heads, kvh = blockIdx.x - tile * a.num_kv_heads;
@@ -491,6 +504,7 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
         if (nb <= a.budget) continue;
         const int first = a.keep_first + blockIdx.y * a.share, last = min(nb - a.keep_last, first + a.share);
         const int32_t *table = block_tables + int64_t(n) * a.max_blocks_per_seq;
+        const bool whole = HERE && nb - a.keep_last - a.keep_first <= a.share;  // one share is all there is
         float size[GROUPS];
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) size[g] = 0.f;
@@ -504,13 +518,14 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
                 for (int j = 0; j < J; ++j) {
                     Op x;
                     x.load(src + 32 * j);
+                    if (x.too_small()) size[g] = INFINITY;
                     plus[g][j] = x.plus();
                     minus[g][j] = x.minus();
                 }
             }
             int b0 = first + 16 * wave;
             int block = b0 < last ? table[min(b0 + r, last - 1)] : 0;
-            for (; b0 < last; b0 += 16 * kWaves) {
+            for (; b0 < last; b0 += 16 * WAVES) {
                 const T *src = bounds + (int64_t(block) * a.num_kv_heads + kvh) * 2 * D + 8 * quad;
                 Op lo[J], hi[J];
 #pragma unroll
@@ -518,7 +533,7 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
                     lo[j].load(src + 32 * j);
                     hi[j].load(src + D + 32 * j);
                 }
-                block = table[min(b0 + 16 * kWaves + r, last - 1)];
+                block = table[min(b0 + 16 * WAVES + r, last - 1)];
                 floatx4 s[GROUPS], up[GROUPS], down[GROUPS];
 #pragma unroll
                 for (int g = 0; g < GROUPS; ++g) s[g] = up[g] = down[g] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -550,10 +565,12 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
                         float *dst = scores + (int64_t(row) * a.num_kv_heads + kvh) * a.stride + b0 - a.keep_first + 4 * quad;
                         if (h0 > 0) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) best[i] = max_of(HERE ? __hip_atomic_load(dst + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : dst[i], best[i]);
+                            for (int i = 0; i < 4; ++i) best[i] = max_of(HERE && whole ? s_scores[b0 - a.keep_first + 4 * quad + i] : HERE ? __hip_atomic_load(dst + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : dst[i], best[i]);
                         }
                         // rows of `stride` have room for whole sets of blocks
-                        if constexpr (HERE) {
+                        if (HERE && whole) {
+                            *reinterpret_cast<floatx4 *>(s_scores + (b0 - a.keep_first + 4 * quad)) = best;
+                        } else if constexpr (HERE) {
 #pragma unroll
                             for (int i = 0; i < 4; ++i) __hip_atomic_store(dst + i, best[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                         } else {
@@ -574,35 +591,46 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(const T *__restr
             const int g = threadIdx.x >> 4, row = row0 + g * set_rows + my_row;
             float x = s_size[0][g][r];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) x = max_of(x, s_size[w][g][r]);
+            for (int w = 1; w < WAVES; ++w) x = max_of(x, s_size[w][g][r]);
             if (my_head == 0 && row < row1) {
                 float *dst = sizes + (int64_t(row) * a.num_kv_heads + kvh) * gridDim.y + blockIdx.y;
-                if (HERE) __hip_atomic_store(dst, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); else *dst = x;
+                if (HERE && whole) s_whole_size = x;
+                else if (HERE) __hip_atomic_store(dst, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                else *dst = x;
             }
         }
         if constexpr (HERE) {
-            // the count may become visible only after the scores: every wavefront waits for its own stores, then all meet
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
             const int compete = nb - a.keep_last - a.keep_first, shares = (compete + a.share - 1) / a.share;
             const int64_t pair = int64_t(row0) * a.num_kv_heads + kvh;
-            if (threadIdx.x == 0) s_last = __hip_atomic_fetch_add(counters + pair * a.counter_step, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
-            __syncthreads();
-            if (!s_last) return;
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");  // the fetches stay behind the count
-            if (threadIdx.x == 0) __hip_atomic_store(counters + pair * a.counter_step, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             float *mine = scores + pair * a.stride;
-            float x[kChoiceMine], most = 0.f;
-            int blocks[kChoiceMine];
-#pragma unroll
-            for (int k = 0; k < kChoiceMine; ++k) {
-                blocks[k] = table[min(a.keep_first + k * kThreads + int(threadIdx.x), nb - 1)];
-                x[k] = __hip_atomic_load(mine + min(k * kThreads + int(threadIdx.x), a.stride - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            float x[MINE], most = 0.f;
+            int blocks[MINE];
+            if (!whole) {
+                // the count may become visible only after the scores: every wavefront waits for its own stores, then all meet
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                if (threadIdx.x == 0) s_last = __hip_atomic_fetch_add(counters + pair * a.counter_step, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
+                __syncthreads();
+                if (!s_last) return;
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");  // the fetches stay behind the count
+                if (threadIdx.x == 0) __hip_atomic_store(counters + pair * a.counter_step, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            } else {
+                __syncthreads();
             }
-            for (int i = threadIdx.x; i < shares; i += kThreads)
-                most = max_of(most, __hip_atomic_load(sizes + pair * gridDim.y + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-            choose<T, D, kThreads, kChoiceMine>(s_choice, x, blocks, most, row0, kvh, compete, a.budget - a.keep_last - a.keep_first, q, bounds, table,
+#pragma unroll
+            for (int k = 0; k < MINE; ++k) {
+                const int i = k * THREADS + int(threadIdx.x);
+                blocks[k] = table[min(a.keep_first + i, nb - 1)];
+                x[k] = whole ? s_scores[i] : __hip_atomic_load(mine + min(i, a.stride - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            if (whole) {
+                most = s_whole_size;
+            } else {
+                for (int i = threadIdx.x; i < shares; i += THREADS)
+                    most = max_of(most, __hip_atomic_load(sizes + pair * gridDim.y + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+            }
+            choose<T, D, THREADS, MINE>(s_choice, x, blocks, most, row0, kvh, compete, a.budget - a.keep_last - a.keep_first, q, bounds, table,
                                                 reinterpret_cast<uint64_t *>(mine), selected + pair * a.budget, a);
             return;
         }
@@ -650,24 +678,29 @@ hipError_t launch_block_select(const void *q, const void *bounds, const int32_t 
         const T *qp = static_cast<const T *>(q), *bp = static_cast<const T *>(bounds);
         if (a.shares > 0) {
             constexpr int kSets = select_sets(sizeof(T) == 4 ? KVC_F32 : KVC_BF16, D);
-            auto launch = [&](auto kernel, int rows) {
+            auto launch = [&](auto kernel, int rows, int threads) {
                 const dim3 grid(unsigned((a.total_q + rows - 1) / rows * a.num_kv_heads), unsigned(a.shares));
-                kernel<<<grid, dim3(kThreads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes, counters, selected, a, rows);
+                kernel<<<grid, dim3(threads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes, counters, selected, a, rows);
             };
             const int set_rows = 16 >> a.heads_log2;
-            if (a.choose_here) launch(block_scores_kernel<T, D, 1, true>, 1);
-            else if (a.total_q > a.num_seqs) launch(block_scores_kernel<T, D, kSets, false>, set_rows * kSets);
-            else launch(block_scores_kernel<T, D, 1, false>, 1);
+            if (a.choose_here && a.max_blocks <= kSmallChoice) launch(block_scores_kernel<T, D, 1, 256, 2>, 1, 256);
+            else if (a.choose_here) launch(block_scores_kernel<T, D, 1, 512, 4>, 1, 512);
+            else if (a.total_q > a.num_seqs) launch(block_scores_kernel<T, D, kSets, kThreads, 0>, set_rows * kSets, kThreads);
+            else launch(block_scores_kernel<T, D, 1, kThreads, 0>, 1, kThreads);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess || a.choose_here) return e;
         }
         auto choose_by = [&](auto kernel, int threads) {
             kernel<<<dim3(unsigned(pairs)), dim3(threads), 0, stream>>>(qp, bp, block_tables, context_lens, q_start, scores, sizes, selected, a);
         };
-        // A wavefront per row where there are many: no barriers (1000 rows, 4 KV heads, up to 500 blocks, both launches, 46.6 us, by
-        // workgroups 52.6; but 24 rows, 2 KV heads, up to 190 blocks 16.4 and 14.4).
-        if (a.max_blocks <= 512 && pairs > 4 * kNumCUs) choose_by(block_choose_kernel<T, D, 64, 8>, 64);
-        else if (a.max_blocks <= kThreads * kChoiceMine) choose_by(block_choose_kernel<T, D, kThreads, kChoiceMine>, kThreads);
+        // Many rows fill the device with small workgroups: a wavefront each up to 512 blocks (1000 rows, 4 KV heads, both launches, 46.6 us, 256
+        // threads each 52.6; 24 rows, 2 KV heads, up to 190 blocks, 16.4 and 14.4), 256 threads up to 2048 (182 rows, 16 KV heads, up to 746 blocks
+        // 29.6 us, 512 threads 34.6).
+        const bool many = pairs > 4 * kNumCUs;
+        if (a.max_blocks <= kSmallChoice && many) choose_by(block_choose_kernel<T, D, 64, 8>, 64);
+        else if (a.max_blocks <= kSmallChoice) choose_by(block_choose_kernel<T, D, 256, 2>, 256);
+        else if (a.max_blocks <= kSelectHereBlocks && many) choose_by(block_choose_kernel<T, D, 256, 8>, 256);
+        else if (a.max_blocks <= kSelectHereBlocks) choose_by(block_choose_kernel<T, D, 512, 4>, 512);
         else choose_by(block_choose_kernel<T, D, 1024, 16>, 1024);
         return hipGetLastError();
     };

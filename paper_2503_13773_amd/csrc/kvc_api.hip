@@ -241,8 +241,7 @@ int check_rows(const kvc_attn_desc *d, int32_t total_q) {
     return total_q < 0 || int64_t(total_q) * d->num_kv_heads >= (int64_t(1) << 32) / kvc::kThreads || chunks > 65535 ? KVC_ERR_BAD_SHAPE : KVC_OK;
 }
 
-constexpr int kSelectHereBlocks = 2048;  // what a workgroup of the scores can choose among
-constexpr int kSelectGroups = 2048;  // workgroups that the scores of few rows are cut into
+constexpr int kSelectGroups = 1024;  // workgroups that the scores of few rows are cut into
 int select_args(const kvc_attn_desc *d, int32_t total_q, int32_t budget, int32_t keep_first, int32_t keep_last, kvc::SelectArgs *a) {
     const int rc = check_rows(d, total_q);
     if (rc != KVC_OK) return rc;
@@ -264,15 +263,19 @@ int select_args(const kvc_attn_desc *d, int32_t total_q, int32_t budget, int32_t
     a->heads_log2 = std::min(4, ilog2(a->group));
     const int compete = a->max_blocks - keep_first - keep_last;
     if (a->max_blocks > budget && budget > keep_first + keep_last) {
-        // rows of chunks are scored several at a time
-        const int64_t tiles = std::max<int64_t>(1, ceil_div(total_q, total_q > d->num_seqs ? kvc::select_sets(d->dtype, d->head_dim) * (16 >> a->heads_log2) : 1) * d->num_kv_heads);
-        const int64_t shares = std::max<int64_t>(1, std::min<int64_t>(ceil_div(compete, 64), kSelectGroups / tiles));
-        a->share = int(ceil_div(ceil_div(compete, shares), 64) * 64);
-        a->shares = int(ceil_div(compete, a->share));
-        a->stride = int(ceil_div(compete, 16) * 32);  // scores of 4 bytes, or of 8 in the same place
         a->counter_step = kvc::counter_step(int64_t(total_q) * d->num_kv_heads);
         a->choose_here = total_q <= d->num_seqs && int64_t(total_q) * d->num_kv_heads <= int64_t(kvc::kWorkspaceHeaderBytes / sizeof(int32_t)) &&
-                         a->max_blocks <= kSelectHereBlocks;
+                         a->max_blocks <= kvc::kSelectHereBlocks;
+        // rows of chunks are scored several at a time
+        const int64_t tiles = std::max<int64_t>(1, ceil_div(total_q, total_q > d->num_seqs ? kvc::select_sets(d->dtype, d->head_dim) * (16 >> a->heads_log2) : 1) * d->num_kv_heads);
+        const int unit = a->choose_here && a->max_blocks > kvc::kSmallChoice ? 128 : 64;  // what its wavefronts score at a time
+        // One workgroup scores all where that is short: nothing to publish and count (two requests of up to 50 blocks, 12 / 12 heads of 64, 7.9 -> 5.6
+        // us; 27 of up to 147, 32 / 8 of 128, 12.1 -> 9.7 us; but six of up to 254 in fp32, 16 / 4 of 128, in shares 11.5, whole 14.8).
+        const bool whole = a->choose_here && compete <= (tiles >= kvc::kNumCUs / 2 ? 256 : d->dtype == KVC_F32 ? 64 : 128);
+        const int64_t shares = whole ? 1 : std::max<int64_t>(1, std::min<int64_t>(ceil_div(compete, unit), kSelectGroups / tiles));
+        a->share = int(ceil_div(ceil_div(compete, shares), unit) * unit);
+        a->shares = int(ceil_div(compete, a->share));
+        a->stride = int(ceil_div(compete, 16) * 32);  // scores of 4 bytes, or of 8 in the same place
     }
     return KVC_OK;
 }

@@ -148,6 +148,8 @@ inline int counter_step(int64_t counters) {
     while (2 * step * counters <= int64_t(kWorkspaceHeaderBytes / sizeof(int32_t)) && step < 32) step *= 2;
     return step;
 }
+constexpr int kSmallChoice = 512;         // blocks among which a workgroup of 256 threads chooses, two a thread
+constexpr int kSelectHereBlocks = 2048;  // blocks among which a workgroup of the scores can choose
 struct SelectArgs {
     int num_seqs, num_q_heads, num_kv_heads, group, block_size_log2, max_blocks_per_seq, max_context_len, total_q;
     int max_blocks;  // blocks of max_context_len

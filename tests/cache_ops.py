@@ -81,14 +81,14 @@ def select(q, bounds_, tables, rows, bs, budget, first, last):
             if nb <= budget:
                 kept = list(range(nb))
             else:
-                scores = []
-                for b in range(first, nb - last):
-                    lo, hi = bounds_[int(tables[n, b]), h].double()
-                    x = q[r, h * group:(h + 1) * group].double()
-                    s = torch.where(x >= 0, x * hi, x * lo)
-                    finite = bool(torch.isfinite(lo).all() and torch.isfinite(hi).all() and torch.isfinite(x).all())
-                    scores.append((-(s.sum(1).max().item() if finite else math.inf), b))
-                kept = sorted(list(range(first)) + [b for _, b in sorted(scores)[:budget - first - last]] + list(range(nb - last, nb)))
+                ids = torch.from_numpy(np.asarray(tables[n, first:nb - last]).astype(np.int64))
+                lo, hi = bounds_[ids, h, 0].double()[:, None], bounds_[ids, h, 1].double()[:, None]
+                x = q[r, h * group:(h + 1) * group].double()[None]
+                score = torch.where(x >= 0, x * hi, x * lo).sum(2).amax(1)
+                finite = torch.isfinite(lo).all(2)[:, 0] & torch.isfinite(hi).all(2)[:, 0] & torch.isfinite(x).all()
+                score = torch.where(finite, score, math.inf)
+                best = torch.sort(score, descending=True, stable=True).indices[:budget - first - last] + first
+                kept = sorted(list(range(first)) + best.tolist() + list(range(nb - last, nb)))
             out[r, h] = kept + [-1] * (budget - len(kept))
     return out
 

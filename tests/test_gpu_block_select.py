@@ -57,6 +57,59 @@ def test_rows_of_chunks(dtype, hq, hkv, d, bs):
     assert (got[:2] == -7).all() and (got[-3:] == -7).all() and (got[2:-3] != -7).any()
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("rows,hkv,blocks", [(300, 4, 300), (260, 5, 700), (30, 2, 1500), (40, 2, 400), (20, 2, 2100)])
+def test_rows_of_chunks_of_every_number_and_length(dtype, d, rows, hkv, blocks):
+    """Few and many rows over short and long tables; zero queries among them, whose scores are all equal, and ones that are not finite."""
+    print(f"[case] select chunks {dtype} x {d} rows {rows} x {hkv} blocks {blocks}", flush=True)
+    rng = np.random.default_rng(blocks)
+    bs = 1 if rows < 100 else 2
+    ctx = [blocks * bs - 3, rows + 2 * bs, blocks * bs - 1]
+    starts = np.array([1, 1 + rows // 2, 1 + rows // 2 + 5, rows])
+    tables, pool = R.scattered(rng, ctx, bs, blocks)
+    q, bounds = _normal(rng, (rows, 3 * hkv, d), dtype), _bounds(rng, pool, hkv, d, dtype)
+    q[3], q[rows - 2, 1] = 0.0, 0.0
+    q[4, 0, 0] = float("inf")
+    bounds[tables[2, 40], hkv - 1, 1, 2] = float("nan")
+    _check(q, bounds, tables, ctx, starts, bs, 24, 1, 2)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("blocks", [60, 130, 300, 511, 513, 2040, 2051, 17000])
+def test_decode_rows_of_every_length(dtype, d, blocks):
+    """One share, several, more than one launch, more than a workgroup holds; equal scores and what is not finite in each."""
+    print(f"[case] select decode {dtype} x {d} blocks {blocks}", flush=True)
+    rng = np.random.default_rng(blocks)
+    ctx, pool = [blocks, blocks - 1, blocks // 2 + 20, blocks, blocks], 500
+    tables = np.stack([rng.integers(0, pool, blocks) for _ in ctx]).astype(np.int32)   # few blocks, many places: scores tie
+    q, bounds = _normal(rng, (5, 6, d), dtype), _bounds(rng, pool, 2, d, dtype)
+    q[3] = 0.0
+    q[4, 5, 1] = float("nan")
+    _check(q, bounds, tables, ctx, None, 1, 20, 2, 1)
+
+
+def test_small_numbers_keep_their_place():
+    """Bounds below the smallest normal number against large queries: products of ordinary size."""
+    rng = np.random.default_rng(12)
+    bs, nb = 16, 200
+    tables = rng.permutation(nb)[None].astype(np.int32)
+    for dtype, tiny, large in (("bf16", 2.0 ** -130, 2.0 ** 120), ("f32", 2.0 ** -140, 2.0 ** 120), ("bf16", 2.0 ** -128, 1.0)):
+        q = (_normal(rng, (1, 4, 128), "f32") * large).to(DTYPES[dtype])
+        bounds = torch.sort(_normal(rng, (nb, 2, 2, 128), "f32") * tiny, dim=2).values.to(DTYPES[dtype])
+        _check(q, bounds, tables, [nb * bs], None, bs, 30, 1, 1)
+    # what tells the blocks apart is tiny beside what they have in common, in the bounds and in the query
+    for first in (True, False):
+        q = _normal(rng, (1, 4, 128), "f32")
+        bounds = torch.sort(_normal(rng, (nb, 2, 2, 128), "f32"), dim=2).values
+        bounds[..., :64] = bounds[:1, ..., :64]
+        if first:
+            q, bounds = q * 2.0 ** 118, torch.cat([bounds[..., :64] * 2.0 ** -118, bounds[..., 64:] * 2.0 ** -134], -1)
+        else:
+            q[..., 64:] *= 2.0 ** -135
+            bounds[..., 64:] *= 2.0 ** 110
+        _check(q, bounds, tables, [nb * bs], None, bs, 30, 1, 1)
+
+
 @pytest.mark.parametrize("ctx,bs,budget", [(30011, 16, 128), (32768, 8, 500), (70000, 16, 64), (9000, 1, 257)])
 def test_long_contexts(ctx, bs, budget):
     print(f"[case] select ctx {ctx} bs {bs} budget {budget}", flush=True)
