@@ -63,7 +63,7 @@ class HipOps:
 
     def __init__(self, num_blocks: int, swap_blocks: int, hq: int, hkv: int, d: int, block_size: int,
                  sparse_budget: Optional[int] = None):
-        """sparse_budget: blocks that a decode query attends to at most (the first one, the last two, the best of the others)."""
+        """sparse_budget: blocks that a decode query attends to at most (of three and more the first one, the last two and the best of the others)."""
         import torch
 
         from . import binding as K
@@ -100,8 +100,9 @@ class HipOps:
     def decode(self, q, tables, lens) -> np.ndarray:
         if self.sparse_budget:
             q, tables, lens = self._bf16(q), self._i32(tables), self._i32(lens)
+            first = min(1, self.sparse_budget - 1)
             kept = self.K.block_select(q, self.bounds, tables, lens, self.sparse_budget, block_size=self.block_size,
-                                       keep_first=min(1, self.sparse_budget - 1), keep_last=min(2, self.sparse_budget))
+                                       keep_first=first, keep_last=min(2, self.sparse_budget - first))
             out = self.K.paged_attention_selected(q, self.pool[0], self.pool[1], tables, lens, kept, self.scale)
             return out.float().cpu().numpy()
         out = self.K.paged_attention_decode(self._bf16(q), self.pool[0], self.pool[1], self._i32(tables),

@@ -179,7 +179,8 @@ def test_the_serving_loop_attends_to_chosen_blocks(oracle_mod):
     assert srv.all_done() and srv.stats["swap_ins"] >= 1 and srv.stats["recomputed"] >= 1
 
 
-def test_the_serving_loop_with_a_small_budget_keeps_what_the_definition_keeps(oracle_mod):
+@pytest.mark.parametrize("budget,first,last", [(1, 0, 1), (2, 1, 1), (4, 1, 2)])
+def test_the_serving_loop_with_a_small_budget_keeps_what_the_definition_keeps(budget, first, last):
     """Each decode call of the loop against the definition on the cache as it is then."""
     from paper_2503_13773_amd.serving import HipOps
     checked = []
@@ -191,12 +192,12 @@ def test_the_serving_loop_with_a_small_budget_keeps_what_the_definition_keeps(or
             rows = [(i, int(c) - 1) for i, c in enumerate(lens)]
             bounds = torch.stack([k.float().amin(2), k.float().amax(2)], 2).to(k.dtype)
             x = torch.from_numpy(np.ascontiguousarray(q).view(np.int16)).view(torch.bfloat16)
-            kept = R.select(x, bounds, tables, rows, S.BS, 4, 1, 2)
+            kept = R.select(x, bounds, tables, rows, S.BS, budget, first, last)
             ref, bound = R.attend(x, k, v, tables, rows, kept, S.SCALE)
             assert (torch.from_numpy(out).double() - ref).abs().sub(bound).max() <= 0
-            checked.append(int((np.asarray(lens) > 4 * S.BS).sum()))
+            checked.append(int((np.asarray(lens) > budget * S.BS).sum()))
             return out
-    srv = S.make_server(Ops(S.NUM_BLOCKS, S.SWAP_BLOCKS, S.HQ, S.HKV, S.D, S.BS, sparse_budget=4))
+    srv = S.make_server(Ops(S.NUM_BLOCKS, S.SWAP_BLOCKS, S.HQ, S.HKV, S.D, S.BS, sparse_budget=budget))
     pending = sorted(S.ARRIVALS, key=lambda a: a[1])
     for it in range(400):
         while pending and pending[0][1] <= it:
