@@ -3,7 +3,12 @@
 //   bounds[block][kv head][0][d] = min_s K[block][kv head][s][d],   bounds[..][1][d] = max_s K[..][s][d],   NaN if one is.
 //
 // Exact in the cache's type: both are values of it.  Bound by memory: K of the filled blocks is read once.  One wavefront per
-// (block, KV head): D * e / 16 lanes cover a token's row, 64 / that tokens per load.
+// (block, KV head): D * e / 16 lanes cover a token's row, 64 / that tokens per load.  Six requests, 8 heads of 128 in bf16, 280 MB of K
+// and bounds: 62.5-64.7 us = 4.3-4.5 TB/s (a copy of 2 GiB moves 5.0 TB/s here); 96 requests, one token each, 4.4 us, the launch.
+//
+// How many tokens are new only the device knows, so a sequence has a bounded number of workgroups, which take its blocks in turn: one per
+// block that the longest can fill would be mostly empty ones in a batch of decode steps with one long prompt (256 requests, one of 8192
+// new tokens: 56.0 us so, 90.8 us with a workgroup per block; the 280 MB above 64.7 us so, 65.5 us with one).
 #include "kvc_internal.h"
 #include "pa_lanes.h"
 
@@ -52,74 +57,81 @@ __device__ inline float most(float a, float b) { return a > b || a != a ? a : b;
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void key_bounds_kernel(const T *__restrict__ k_cache, T *__restrict__ bounds, const int32_t *__restrict__ block_tables,
                                                               const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start,
-                                                              int blocks_per_seq, int num_kv_heads, int block_size_log2, int max_blocks_per_seq,
+                                                              int groups_per_seq, int num_kv_heads, int block_size_log2, int max_blocks_per_seq,
                                                               int num_pool_blocks) {
     constexpr int N = Word<T>::N, LR = D / N, TOKENS = 64 / LR;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int h = blockIdx.y * kWaves + wave;
     if (h >= num_kv_heads) return;
-    const int n = blockIdx.x / blocks_per_seq, bs = 1 << block_size_log2;
+    const int n = blockIdx.x / groups_per_seq, bs = 1 << block_size_log2;
     const int ctx = context_lens[n], fresh = q_start ? q_start[n + 1] - q_start[n] : 1;
     if (fresh <= 0 || ctx < bs) return;
-    const int j = (max(ctx - fresh, 0) >> block_size_log2) + int(blockIdx.x - n * blocks_per_seq);
-    if (j >= min(ctx >> block_size_log2, max_blocks_per_seq)) return;
-    const int block = block_tables[int64_t(n) * max_blocks_per_seq + j];
-    if (block < 0 || block >= num_pool_blocks) return;
-    const int c = lane % LR, t0 = lane / LR;
-    const int64_t at = int64_t(block) * num_kv_heads + h;
-    const uint4 *src = reinterpret_cast<const uint4 *>(k_cache + (at << block_size_log2) * D);
-    float lo[N], hi[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        lo[i] = INFINITY;
-        hi[i] = -INFINITY;
-    }
-    constexpr int U = 4;
-    for (int t = 0; t < bs; t += U * TOKENS) {
-        uint4 w[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = src[min(t + u * TOKENS + t0, bs - 1) * LR + c];  // past the end: the last one again
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float x[N];
-            Word<T>::get(w[u], x);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                lo[i] = least(lo[i], x[i]);
-                hi[i] = most(hi[i], x[i]);
-            }
-        }
-    }
-#pragma unroll
-    for (int off = LR; off < 64; off <<= 1) {
+    const int c = lane % LR, t0 = lane / LR, end = min(ctx >> block_size_log2, max_blocks_per_seq);
+    const int32_t *table = block_tables + int64_t(n) * max_blocks_per_seq;
+    int j = (max(ctx - fresh, 0) >> block_size_log2) + int(blockIdx.x - n * groups_per_seq);
+    int next = j < end ? table[j] : -1;
+    for (; j < end; j += groups_per_seq) {
+        const int block = next;
+        next = j + groups_per_seq < end ? table[j + groups_per_seq] : -1;
+        if (block < 0 || block >= num_pool_blocks) continue;
+        const int64_t at = int64_t(block) * num_kv_heads + h;
+        const uint4 *src = reinterpret_cast<const uint4 *>(k_cache + (at << block_size_log2) * D);
+        float lo[N], hi[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            lo[i] = least(lo[i], __shfl_xor(lo[i], off));
-            hi[i] = most(hi[i], __shfl_xor(hi[i], off));
+            lo[i] = INFINITY;
+            hi[i] = -INFINITY;
         }
+        constexpr int U = 4;
+        for (int t = 0; t < bs; t += U * TOKENS) {
+            uint4 w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) w[u] = src[min(t + u * TOKENS + t0, bs - 1) * LR + c];  // past the end: the last one again
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float x[N];
+                Word<T>::get(w[u], x);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    lo[i] = least(lo[i], x[i]);
+                    hi[i] = most(hi[i], x[i]);
+                }
+            }
+        }
+#pragma unroll
+        for (int off = LR; off < 64; off <<= 1) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                lo[i] = least(lo[i], __shfl_xor(lo[i], off));
+                hi[i] = most(hi[i], __shfl_xor(hi[i], off));
+            }
+        }
+        uint4 *dst = reinterpret_cast<uint4 *>(bounds + at * 2 * D);
+        if (t0 == 0) dst[c] = Word<T>::put(lo);
+        if (t0 == 1) dst[LR + c] = Word<T>::put(hi);
     }
-    uint4 *dst = reinterpret_cast<uint4 *>(bounds + at * 2 * D);
-    if (t0 == 0) dst[c] = Word<T>::put(lo);
-    if (t0 == 1) dst[LR + c] = Word<T>::put(hi);
 }
 
 }  // namespace
+
+constexpr int64_t kMostBoundsGroups = 8192;  // of all sequences, for each four KV heads
 
 hipError_t launch_key_bounds(const void *k_cache, void *bounds, const int32_t *block_tables, const int32_t *context_lens, const int32_t *q_start,
                              const kvc_attn_desc &d, int block_size_log2, int max_query_len, hipStream_t stream) {
     // blocks that `max_query_len` tokens can fill
     const int64_t blocks = std::min<int64_t>((int64_t(max_query_len) >> block_size_log2) + 1, d.max_blocks_per_seq);
+    const int64_t groups = std::min<int64_t>(blocks, (kMostBoundsGroups + d.num_seqs - 1) / d.num_seqs);
     const int64_t heads = (d.num_kv_heads + kWaves - 1) / kWaves;
     constexpr int64_t kMostGroups = (int64_t(1) << 32) / kThreads - 1;
-    const int64_t most = kMostGroups / (blocks * heads);
+    const int64_t most = kMostGroups / (groups * heads);
     if (most == 0 || heads > 65535) return hipErrorInvalidValue;
     for (int64_t n = 0; n < d.num_seqs; n += most) {
         const int64_t seqs = d.num_seqs - n < most ? d.num_seqs - n : most;
-        const dim3 grid(unsigned(seqs * blocks), unsigned(heads));
+        const dim3 grid(unsigned(seqs * groups), unsigned(heads));
         auto launch = [&](auto kernel, auto type) {
             using T = decltype(type);
             kernel<<<grid, dim3(kThreads), 0, stream>>>(static_cast<const T *>(k_cache), static_cast<T *>(bounds), block_tables + n * d.max_blocks_per_seq,
-                                                        context_lens + n, q_start ? q_start + n : nullptr, int(blocks), d.num_kv_heads, block_size_log2,
+                                                        context_lens + n, q_start ? q_start + n : nullptr, int(groups), d.num_kv_heads, block_size_log2,
                                                         d.max_blocks_per_seq, d.num_pool_blocks);
         };
         if (d.dtype == KVC_F32) {

@@ -118,6 +118,14 @@ def test_bounds_of_filled_blocks(dtype, hkv, d, bs):
     _bounds_case(dtype, hkv, d, bs, ctx, ctx, 5, special=True)
 
 
+@pytest.mark.parametrize("n", [300, 9000])
+def test_bounds_of_a_long_prompt_among_many_decode_steps(n):
+    """More blocks than a sequence has workgroups, and more sequences than the launch would have in all."""
+    ctx, new = np.full(n, 5), np.ones(n, dtype=np.int64)
+    ctx[::3], ctx[7], new[7] = 4, 1500, 1499
+    _bounds_case("bf16", 5, 64, 4, ctx, new, 6)
+
+
 def test_bounds_without_work_and_outside_the_pool():
     import paper_2503_13773_amd as K
     k = torch.randn((4, 2, 16, 64), device="cuda")
