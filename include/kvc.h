@@ -417,8 +417,9 @@ KVC_API int kvc_key_bounds_update(const void *k_cache, void *bounds, const int32
  *   - Positions at or past max_context_len are taken for the last one below it.
  *   - workspace: device memory, 256-byte aligned, kvc_block_select_workspace_bytes(desc, total_q, ...) of it (may be NULL when
  *     that is 0), with the counter header and the rules of kvc_paged_attention_decode's workspace: prepared once by
- *     kvc_paged_attention_decode_workspace_init, and one workspace that is large enough may serve all of these calls.  Calls that
- *     share one must not overlap in time.
+ *     kvc_paged_attention_decode_workspace_init, and one workspace that is large enough may serve all of these calls: what is
+ *     reported for a call does for fewer rows, blocks or tokens too.  Calls that share one must not overlap in time.
+ *   - The entries of block_tables up to a row's own block must lie in the pool (of those above the budget they are read).
  */
 KVC_API size_t kvc_block_select_workspace_bytes(const kvc_attn_desc *desc, int32_t total_q, int32_t budget, int32_t keep_first,
                                                 int32_t keep_last);
@@ -435,8 +436,10 @@ KVC_API int kvc_block_select(const void *q, const void *bounds, const int32_t *b
  * sequence are left as they were.  Accumulation is fp32, output rounded to nearest even.
  *   - workspace: device memory, 256-byte aligned, kvc_paged_attention_selected_workspace_bytes(desc, total_q, budget) of it (may be
  *     NULL when that is 0), with the counter header and the rules of kvc_paged_attention_decode's workspace: prepared once by
- *     kvc_paged_attention_decode_workspace_init, and one workspace that is large enough may serve both.  Calls that share one must
- *     not overlap in time.
+ *     kvc_paged_attention_decode_workspace_init, and one workspace that is large enough may serve both: what is reported for a
+ *     call does for fewer rows and shorter lists too, also where that call itself needs nothing, and a call is refused only for what it
+ *     needs itself.  Calls that share one must not overlap in time.
+ *   - The table entries that a list names, and that of the row's own block, must lie in the pool.
  */
 KVC_API size_t kvc_paged_attention_selected_workspace_bytes(const kvc_attn_desc *desc, int32_t total_q, int32_t budget);
 KVC_API int kvc_paged_attention_selected(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables,

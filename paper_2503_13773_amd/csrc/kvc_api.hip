@@ -263,6 +263,9 @@ int select_args(const kvc_attn_desc *d, int32_t total_q, int32_t budget, int32_t
     a->heads_log2 = std::min(4, ilog2(a->group));
     const int compete = a->max_blocks - keep_first - keep_last;
     if (a->max_blocks > budget && budget > keep_first + keep_last) {
+        // a row's scores are indexed in 32 bits, and a workgroup of 1024 threads chooses among many blocks
+        if (ceil_div(compete, 16) * 32 > INT32_MAX || (a->max_blocks > kvc::kSelectHereBlocks && int64_t(total_q) * d->num_kv_heads >= (int64_t(1) << 32) / 1024))
+            return KVC_ERR_BAD_SHAPE;
         a->counter_step = kvc::counter_step(int64_t(total_q) * d->num_kv_heads);
         a->choose_here = total_q <= d->num_seqs && int64_t(total_q) * d->num_kv_heads <= int64_t(kvc::kWorkspaceHeaderBytes / sizeof(int32_t)) &&
                          a->max_blocks <= kvc::kSelectHereBlocks;
@@ -281,23 +284,31 @@ int select_args(const kvc_attn_desc *d, int32_t total_q, int32_t budget, int32_t
 }
 // Counters, scores of all blocks that compete, and how large the sums behind them can be.
 size_t select_bytes(const kvc::SelectArgs &a, int32_t total_q) {
-    return a.shares == 0 || total_q == 0 ? 0 : kvc::kWorkspaceHeaderBytes + size_t(total_q) * a.num_kv_heads * (a.stride + a.shares) * sizeof(float);
+    // room for as many shares as there can be (of 64 blocks at least), so that what does for more blocks or rows does for fewer, whose shares
+    // can be more
+    return a.shares == 0 || total_q == 0 ? 0 : kvc::kWorkspaceHeaderBytes + size_t(total_q) * a.num_kv_heads * (size_t(a.stride) + a.stride / 32) * sizeof(float);
 }
 
 // How attention over chosen blocks is cut.  All lists are equally long as far as the host knows.
 struct SelectedPlan {
     kvc::SelectedArgs a;
-    uint64_t ml_offset, bytes;  // of the workspace: counters, then the parts' accumulators, then their maxima and sums
+    uint64_t ml_offset, need;  // of the workspace: counters, then the parts' accumulators, then their maxima and sums
+    uint64_t bytes;            // asked for: does for fewer rows and shorter lists too
 };
 // Units of up to half a compute unit each are cut into kSelectedGroups workgroups in all, more are not cut: 256 units of 32 long documents, 64 / 8
 // heads of 128, 43.3 us whole with eight wavefronts, in two parts each 47.5 (but 96 of up to 512 tokens 9.3 in parts, whole 10.7).  Eight wavefronts
 // up to kSelectedFewUnits and for the 256: one document 9.1 us, with four 9.6; 64 units 17.5 with four, with eight 21.5.
 constexpr int kSelectedGroups = 512;
 constexpr int kSelectedFewUnits = 32;
+constexpr int kValuTripBytes = 4 * 4096;  // of K, by four wavefronts of the vector-ALU kernel
 // Rows of chunks: from here on a wavefront takes a unit (1000 rows, 32 / 8 heads of 64: 93 us, by workgroups 171; 200 rows, 32 / 8 heads of 128
 // 19.8 and 25.7; but 136 rows 18.8 and 19.6, 240 rows of heads of 64 33.5 and 31.7).  Not in a decode step, whose units share nothing (150
 // requests, 134 and 115 us).
 constexpr int kSelectedManyUnits = 1024;
+// A decode step's units share no blocks, so their loads pass through the caches: 32 long documents 45.6 us, as loads that stay 53.3; 16 requests of 1024
+// tokens, 128 units, 17.5 and 18.4; 64 of heads of 64, 512 units, 23.4 and 23.1.  Up to 8 units it is the other way around, 9.4 us staying, 10.0
+// passing through (16 units 11.7 through, 11.9 staying).
+constexpr int kSelectedStayUnits = 8;
 int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, SelectedPlan *pl) {
     const int rc = check_rows(d, total_q);
     if (rc != KVC_OK) return rc;
@@ -325,6 +336,7 @@ int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, 
         a.units_per_block_log2 = a.block_size_log2 - a.unit_log2;
         a.tiles = int(ceil_div(int64_t(budget) << a.block_size_log2, 32));
         a.wave_per_unit = total_q > d->num_seqs && units >= kSelectedManyUnits;
+        a.again = total_q > d->num_seqs || units <= kSelectedStayUnits;
         a.waves = units <= kSelectedFewUnits || (units > kvc::kNumCUs / 2 && units <= kvc::kNumCUs) ? 8 : 4;
         trip = a.waves;
     } else {
@@ -332,7 +344,7 @@ int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, 
         // Tokens that four wavefronts take at once, 4 KiB of K each.  Sixteen where they all fit the device, have more than two such trips to
         // make (fp32, 16 / 4 heads, 33 lists of 256 tokens of 128, us with four / sixteen: 17.3 / 12.3, one of 1024 tokens of 64 13.1 / 10.7; 45
         // of 128 of 64, two trips, 6.3 / 7.5), and the registers allow it (four heads in bf16 spill).
-        const int tokens = 4 * 4096 / (d->head_dim * (d->dtype == KVC_F32 ? 4 : 2));
+        const int tokens = kValuTripBytes / (d->head_dim * (d->dtype == KVC_F32 ? 4 : 2));
         const bool wide = units <= kvc::kNumCUs && (int64_t(budget) << a.block_size_log2) > 2 * tokens && (d->dtype == KVC_F32 || heads < 4);
         a.waves = wide ? 16 : 4;
         trip = std::max(1, (tokens * a.waves / 4) >> a.block_size_log2);
@@ -341,12 +353,20 @@ int make_selected_plan(const kvc_attn_desc *d, int32_t total_q, int32_t budget, 
     const int64_t parts = units > 0 ? std::max<int64_t>(1, std::min<int64_t>((units > kvc::kNumCUs / 2 || !a.on_mfma ? kvc::kNumCUs : kSelectedGroups) / units, most)) : 1;
     a.tiles_per_part = int(ceil_div(a.tiles, parts));
     a.parts = int(ceil_div(a.tiles, a.tiles_per_part));
-    pl->ml_offset = pl->bytes = 0;
+    pl->ml_offset = pl->need = pl->bytes = 0;
     a.counter_step = kvc::counter_step(units);
+    const uint64_t slot_heads = a.on_mfma ? 16 : heads, slot_floats = slot_heads * d->head_dim;
     if (a.parts > 1) {
-        const uint64_t slots = uint64_t(units) * a.parts, slot_heads = a.on_mfma ? 16 : heads;
-        pl->ml_offset = kvc::kWorkspaceHeaderBytes + slots * slot_heads * d->head_dim * sizeof(float);
-        pl->bytes = pl->ml_offset + slots * slot_heads * 2 * sizeof(float);
+        pl->ml_offset = kvc::kWorkspaceHeaderBytes + uint64_t(units) * a.parts * slot_floats * sizeof(float);
+        pl->need = pl->ml_offset + uint64_t(units) * a.parts * slot_heads * 2 * sizeof(float);
+    }
+    // What a call needs falls to nothing as its units fill the device by themselves; what is asked for does not: room for as many parts as any
+    // smaller call is cut into.
+    const int64_t least_trip = a.on_mfma ? 4 : std::max<int64_t>(1, kValuTripBytes / (int64_t(d->head_dim) * (d->dtype == KVC_F32 ? 4 : 2)) >> a.block_size_log2);
+    const int64_t most_parts = std::min<int64_t>(kvc::kMaxSelectedParts, ceil_div(a.tiles, least_trip));
+    if (units > 0 && most_parts > 1) {
+        const uint64_t slots = std::min<int64_t>(kSelectedGroups, units * most_parts);
+        pl->bytes = kvc::kWorkspaceHeaderBytes + slots * (slot_floats + 2 * slot_heads) * sizeof(float);
     }
     return KVC_OK;
 }
@@ -1047,10 +1067,10 @@ int kvc_paged_attention_selected(const void *q, const void *k_cache, const void 
     if (!selected) return KVC_ERR_NULL;
     rc = check_attn_args(q, k_cache, v_cache, block_tables, context_lens, scale, out);
     if (rc != KVC_OK) return rc;
-    if (pl.bytes > 0 && (!workspace || workspace_bytes < pl.bytes)) return KVC_ERR_WORKSPACE;
+    if (pl.need > 0 && (!workspace || workspace_bytes < pl.need)) return KVC_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return KVC_ERR_ALIGN;
     kvc::Workspace ws = {nullptr, nullptr, nullptr};
-    if (pl.bytes > 0) {
+    if (pl.need > 0) {
         char *base = static_cast<char *>(workspace);
         ws = {reinterpret_cast<float *>(base + kvc::kWorkspaceHeaderBytes), reinterpret_cast<float *>(base + pl.ml_offset), reinterpret_cast<int32_t *>(base)};
     }

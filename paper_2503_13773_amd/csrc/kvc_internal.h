@@ -168,8 +168,9 @@ constexpr int kMaxSelectedParts = 64;  // parts a list is cut into at most
 struct SelectedArgs {
     int num_seqs, num_q_heads, num_kv_heads, group, block_size_log2, max_blocks_per_seq, max_context_len, budget, total_q;
     float scale, scale_log2e;
-    // how the work is cut: wavefronts of a workgroup, heads of a KV head in a unit, tiles of a list (vector ALUs: entries), parts of a list and tiles of one
-    int on_mfma, wave_per_unit, waves, heads_per_chunk, unit_log2, units_per_block_log2, tiles, parts, tiles_per_part;
+    // how the work is cut: whether units near each other share blocks, wavefronts of a workgroup, heads of a KV head in a unit, tiles of a list (vector
+    // ALUs: entries), parts of a list and tiles of one
+    int on_mfma, wave_per_unit, again, waves, heads_per_chunk, unit_log2, units_per_block_log2, tiles, parts, tiles_per_part;
     int counter_step;  // counters of units lie so many words apart
 };
 hipError_t launch_attention_selected(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables, const int32_t *context_lens,

@@ -10,7 +10,7 @@
 //   more: a workgroup per unit, whose wavefronts take the tiles of the list in turn and meet in LDS;
 //   many: a wavefront per unit, nothing to join.
 //
-// Bound: memory in a decode batch (32 long documents, 64 / 8 heads of 128 in bf16, 128 blocks of 16 each, 269 MB: 52 us = 5.2 TB/s; a
+// Bound: memory in a decode batch (32 long documents, 64 / 8 heads of 128 in bf16, 128 blocks of 16 each, 269 MB: 45.6 us = 5.9 TB/s; a
 // copy of 2 GiB moves 5.0 TB/s here); launch and the join for a single row (9.4 us); LDS and the issue of instructions for chunks, whose rows
 // read the same blocks again from L2 (1000 rows, 32 / 8 heads of 64, 1024 tokens each: 91-93 us, 2.1 GB through LDS).
 #include "cache_rows.h"
@@ -116,7 +116,8 @@ struct ListOf {
 
 // Tiles first, first + step, ... below `tiles` of a list's part that begins at tile0.  Whether any token counted.  A lane holds the place of
 // one unit; 64 >> units_log2 tiles are known at a time.  UNIFORM: the rows of a load lie in one unit (blocks of 8 tokens and more at
-// head_dim 64, all at 128).  AGAIN: rows near this one read the same blocks, so loads leave them in L2.
+// head_dim 64, all at 128).  AGAIN: rows near this one read the same blocks, so loads leave them in L2 (else they
+// pass through it).
 // `stage`: K and V of a tile, this wavefront's own.
 template <int HD, bool UNIFORM, bool AGAIN>
 __device__ inline bool attend_list(State<HD> &st, const bf16x8 (&qb)[HD / 32], const uint16_t *__restrict__ k_cache, const uint16_t *__restrict__ v_cache,
@@ -328,7 +329,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void pa_selected_mfma_kernel(
     State<HD> st;
     st.reset();
     const int tile0 = part * a.tiles_per_part;
-    const bool any = attend_list<HD, UNIFORM, true>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, tile0,
+    const bool any = attend_list<HD, UNIFORM, AGAIN>(st, qb, k_cache, v_cache, list_of(a, u, selected, block_tables), a.scale_log2e, tile0,
                                               min(a.tiles_per_part, a.tiles - tile0), wave, WAVES, s_stage[wave]);
     st.finish();
     // a wavefront or part without a token says so with a maximum of -inf (with tokens it is -FLT_MAX at least)
@@ -685,8 +686,8 @@ hipError_t launch_attention_selected(const void *q, const void *k_cache, const v
             };
 #define KVC_PARTS(HD, UNIFORM)                                                                                                     \
     do {                                                                                                                           \
-        if (a.waves == 8) q_start ? launch(pa_selected_mfma_kernel<HD, UNIFORM, true, 8>) : launch(pa_selected_mfma_kernel<HD, UNIFORM, false, 8>); \
-        else q_start ? launch(pa_selected_mfma_kernel<HD, UNIFORM, true, 4>) : launch(pa_selected_mfma_kernel<HD, UNIFORM, false, 4>); \
+        if (a.waves == 8) a.again ? launch(pa_selected_mfma_kernel<HD, UNIFORM, true, 8>) : launch(pa_selected_mfma_kernel<HD, UNIFORM, false, 8>); \
+        else a.again ? launch(pa_selected_mfma_kernel<HD, UNIFORM, true, 4>) : launch(pa_selected_mfma_kernel<HD, UNIFORM, false, 4>);               \
     } while (0)
             if (head_dim == 64) { if (uniform) KVC_PARTS(64, true); else KVC_PARTS(64, false); }
             else KVC_PARTS(128, true);

@@ -125,3 +125,41 @@ def test_paged_attention_selected(K):
         assert call(**kw) == NULL, kw
     for kw in (dict(q=P + 8), dict(k=P + 2), dict(v=P + 4), dict(out=P + 8)):
         assert call(**kw) == ALIGN, kw
+
+
+def test_lists_of_scores_that_do_not_fit(K):
+    """Rows of scores are indexed in 32 bits, and many blocks are chosen among by 1024 threads a row."""
+    def need(rows, **kw):
+        return K.lib().kvc_block_select_workspace_bytes(ctypes.byref(desc(K, **kw)), rows, 8, 1, 1)
+    for blocks, fits in ((1 << 30, False), ((1 << 30) - 32, True)):
+        d = desc(K, block_size=1, max_blocks_per_seq=blocks)
+        assert (need(9, block_size=1, max_blocks_per_seq=blocks) > 0) == fits
+        rc = K.lib().kvc_block_select(P, 2 * P, 3 * P, 4 * P, 5 * P, 6 * P, 8, 1, 1, ctypes.byref(d), 9, None, 0, None)
+        assert rc == (WORKSPACE if fits else SHAPE)
+    hkv = desc(K).num_kv_heads
+    for blocks, rows, fits in ((2049, (1 << 22) // hkv, False), (2049, ((1 << 22) - 1) // hkv, True), (2048, (1 << 22) // hkv, True)):
+        assert (need(rows, max_blocks_per_seq=blocks) > 0) == fits
+
+
+def test_a_workspace_does_for_smaller_calls(K):
+    """Fewer rows, blocks and kept blocks have more shares and parts each; what was asked for before has room for them."""
+    for dtype in (K.KVC_F32, K.KVC_BF16):
+        def select(rows, blocks, first=0):
+            d = desc(K, dtype=dtype, num_seqs=rows, num_q_heads=8, num_kv_heads=1, max_blocks_per_seq=blocks)
+            return K.lib().kvc_block_select_workspace_bytes(ctypes.byref(d), rows, 8, first, 1)
+        for rows in (1, 2, 8, 9, 1024, 1025):
+            sizes = [select(rows, b) for b in (9, 10, 64, 65, 129, 130, 513, 514, 2048, 2049, 8193, 8194, 65537, 65538, 65539)]
+            assert sizes == sorted(sizes) and all(select(rows, b, 3) <= select(rows, b) for b in (65538, 65541, 8194, 8197))
+        for blocks in (10, 65538):
+            sizes = [select(rows, blocks) for rows in range(1, 1100, 7)]
+            assert sizes == sorted(sizes)
+        for block_size, hq in ((16, 8), (1, 8), (64, 2), (16, 40)):
+            def selected(rows, budget):
+                d = desc(K, dtype=dtype, num_seqs=rows, num_q_heads=hq, num_kv_heads=2, block_size=block_size, max_blocks_per_seq=4096)
+                return K.lib().kvc_paged_attention_selected_workspace_bytes(ctypes.byref(d), rows, budget)
+            for budget in (1, 4, 40, 128, 2000):
+                sizes = [selected(rows, budget) for rows in (1, 2, 3, 8, 16, 17, 32, 64, 65, 128, 129, 1000)]
+                assert sizes == sorted(sizes)
+            for rows in (1, 40, 1000):
+                sizes = [selected(rows, budget) for budget in (1, 2, 3, 8, 9, 32, 33, 100, 128, 2000, 4096)]
+                assert sizes == sorted(sizes)

@@ -180,3 +180,34 @@ def test_refusals():
                selected=torch.zeros((3, 2, 3), dtype=torch.int32, device="cuda"))):
         with pytest.raises((K.KvcError, ValueError)):
             K.paged_attention_selected(**{**ok, **kw})
+
+
+def test_a_workspace_of_a_larger_batch_serves_smaller_ones():
+    """A batch that needs none itself; smaller ones, whose lists are cut into parts, use what was asked for it."""
+    import paper_2503_13773_amd as K
+    print("[case] selected workspace of a larger batch", flush=True)
+    rng = np.random.default_rng(12)
+    hq, hkv, d, bs, budget = 8, 2, 128, 16, 40
+    for dtype in ("bf16", "f32"):
+        ws = K.new_selected_workspace(torch.zeros((300, hq, d), dtype=DTYPES[dtype], device="cuda"), torch.zeros((9, hkv, bs, d), dtype=DTYPES[dtype], device="cuda"),
+                                      torch.zeros((300, 50), dtype=torch.int32, device="cuda"), budget)
+        for rows in (300, 150, 65, 9, 1):
+            ctx = [int(x) for x in rng.integers(30 * bs, 50 * bs, rows)]
+            tables, pool = np.stack([rng.permutation(60)[:50] for _ in ctx]).astype(np.int32), 60
+            q, k, v = _normal(rng, (rows, hq, d), dtype), _normal(rng, (pool, hkv, bs, d), dtype), _normal(rng, (pool, hkv, bs, d), dtype)
+            selected = R.some_lists(rng, R.rows_of(ctx, None, rows), hkv, bs, budget, False)
+            _check(q, k, v, tables, ctx, None, selected, 1 / math.sqrt(d), workspace=ws)
+    assert not ws[:4096].any()
+
+
+@pytest.mark.parametrize("d,bs", [(128, 16), (64, 32), (64, 4)])
+def test_decode_rows_on_both_sides_of_the_loads_that_stay(d, bs):
+    """Rows of eight units and of more, of up to a device full, in four and eight wavefronts each."""
+    rng = np.random.default_rng(13)
+    for rows in (4, 5, 20, 40, 70, 129, 160):
+        print(f"[case] selected decode rows {rows} x {d} bs {bs}", flush=True)
+        ctx = [int(x) for x in rng.integers(0, 40 * bs, rows)]
+        tables = np.stack([rng.permutation(60)[:40] for _ in ctx]).astype(np.int32)
+        q, k, v = _normal(rng, (rows, 6, d), "bf16"), _normal(rng, (60, 2, bs, d), "bf16"), _normal(rng, (60, 2, bs, d), "bf16")
+        selected = R.some_lists(rng, R.rows_of(ctx, None, rows), 2, bs, 19, True)
+        _check(q, k, v, tables, ctx, None, selected, 0.1)
