@@ -4,11 +4,11 @@
 //
 // Exact in the cache's type: both are values of it.  Bound by memory: K of the filled blocks is read once.  One wavefront per
 // (block, KV head): D * e / 16 lanes cover a token's row, 64 / that tokens per load.  Six requests, 8 heads of 128 in bf16, 280 MB of K
-// and bounds: 62.5-64.7 us = 4.3-4.5 TB/s (a copy of 2 GiB moves 5.0 TB/s here); 96 requests, one token each, 4.4 us, the launch.
+// and bounds: 54.8 us = 5.1 TB/s (a copy of 2 GiB moves 5.0 TB/s here; loads that leave K in the caches 62.3 us); 96 requests, one token each, 4.4 us, the launch.
 //
 // How many tokens are new only the device knows, so a sequence has a bounded number of workgroups, which take its blocks in turn: one per
 // block that the longest can fill would be mostly empty ones in a batch of decode steps with one long prompt (256 requests, one of 8192
-// new tokens: 56.0 us so, 90.8 us with a workgroup per block; the 280 MB above 64.7 us so, 65.5 us with one).
+// new tokens: 56.0 us so, 90.8 us with a workgroup per block; the 280 MB above were 64.7 and 65.5 us).
 #include "kvc_internal.h"
 #include "pa_lanes.h"
 
@@ -54,6 +54,11 @@ struct Word<uint16_t> {
 __device__ inline float least(float a, float b) { return a < b || a != a ? a : b; }
 __device__ inline float most(float a, float b) { return a > b || a != a ? a : b; }
 
+__device__ inline uint4 once(const uint4 *p) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)));
+}
+
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void key_bounds_kernel(const T *__restrict__ k_cache, T *__restrict__ bounds, const int32_t *__restrict__ block_tables,
                                                               const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start,
@@ -86,7 +91,7 @@ __global__ __launch_bounds__(kThreads) void key_bounds_kernel(const T *__restric
         for (int t = 0; t < bs; t += U * TOKENS) {
             uint4 w[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) w[u] = src[min(t + u * TOKENS + t0, bs - 1) * LR + c];  // past the end: the last one again
+            for (int u = 0; u < U; ++u) w[u] = once(src + min(t + u * TOKENS + t0, bs - 1) * LR + c);  // past the end: the last one again
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 float x[N];
