@@ -22,14 +22,15 @@
 // Scores and choice are two launches.  A decode batch of at most 1024 (row, KV head) pairs and 2048 blocks has a workgroup or a few per
 // pair and the last one to finish a pair's scores chooses at once, which saves the second launch.
 //
-// Bound: the bounds' bytes in a decode batch, read in pieces of 2 * D * e (32 long documents, 64 / 8 heads of 128, 172 MB: 43 us with
-// what the reader keeps in its caches, 54 us without); the chain of dependent phases where there are few rows (one document of 30 011 tokens:
-// 11.7 us, of which the choice is 4.5); products and LDS for chunks, whose rows share the bounds (1000 rows, 16 / 4 heads of 64 in fp32:
+// Bound: the bounds' bytes in a decode batch, read in pieces of 2 * D * e (32 long documents, 64 / 8 heads of 128, 172 MB:
+// 44.6 us = 3.85 TB/s); the chain of dependent phases where there are few rows (one document of 30 011 tokens:
+// 10.8 us, of which the choice is 4.5); products and LDS for chunks, whose rows share the bounds (1000 rows, 16 / 4 heads of 64 in fp32:
 // 34 us of scores, 13 us of choice).
 #include <type_traits>
 
 #include "cache_rows.h"
 #include "kvc_internal.h"
+#include "lds_loads.h"
 #include "pa_mfma_tile.h"
 
 namespace kvc {
@@ -80,6 +81,9 @@ template <>
 struct Operand<uint16_t> {
     uint4 w;
     __device__ void load(const uint16_t *p) { w = *reinterpret_cast<const uint4 *>(p); }
+    // from a stage's row, whose 16-byte chunk c lies at place(c)
+    template <class Place>
+    __device__ void load(const unsigned char *row, int first, Place place) { w = *reinterpret_cast<const uint4 *>(row + place(first / 8)); }
     __device__ bool too_small() const { return false; }
     __device__ static uint32_t negative(uint32_t x) { return ((x >> 15) & 0x10001u) * 0xffffu; }
     __device__ Operand plus() const { return {uint4{w.x & ~negative(w.x), w.y & ~negative(w.y), w.z & ~negative(w.z), w.w & ~negative(w.w)}}; }
@@ -101,10 +105,14 @@ template <>
 struct Operand<float> {
     float x[8];
     bf16x8 hi, lo;
-    __device__ void load(const float *p) {
-        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+    __device__ void load(const float *p) { take(*reinterpret_cast<const float4 *>(p), *reinterpret_cast<const float4 *>(p + 4)); }
+    __device__ void take(const float4 &a, const float4 &b) {
         x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
         x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+    template <class Place>
+    __device__ void load(const unsigned char *row, int first, Place place) {
+        take(*reinterpret_cast<const float4 *>(row + place(first / 4)), *reinterpret_cast<const float4 *>(row + place(first / 4 + 1)));
     }
     __device__ bool too_small() const {
         bool any = false;
@@ -481,7 +489,7 @@ __device__ inline void choose(Choice<THREADS / 64, MINE> &s, float (&x)[MINE], c
 // sizes travel by device-scope accesses; each workgroup waits for its own and counts itself; nobody waits for anybody.  A single share's
 // scores stay in LDS.
 template <class T, int D, int GROUPS, int THREADS, int MINE>
-__global__ __launch_bounds__(THREADS) void block_scores_kernel(const T *__restrict__ q, const T *__restrict__ bounds, const int32_t *__restrict__ block_tables,
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && MINE > 0 ? 4 : 1) void block_scores_kernel(const T *__restrict__ q, const T *__restrict__ bounds, const int32_t *__restrict__ block_tables,
                                                                 const int32_t *__restrict__ context_lens, const int32_t *__restrict__ q_start,
                                                                 float *__restrict__ scores, float *__restrict__ sizes, int32_t *__restrict__ counters,
                                                                 int32_t *__restrict__ selected, SelectArgs a, int tile_rows) {
@@ -489,7 +497,16 @@ __global__ __launch_bounds__(THREADS) void block_scores_kernel(const T *__restri
     constexpr bool HERE = MINE > 0;
     using Op = Operand<T>;
     __shared__ float s_size[WAVES][GROUPS][16];
-    __shared__ std::conditional_t<HERE, Choice<WAVES, HERE ? MINE : 1>, int> s_choice;
+    using Chosen = std::conditional_t<HERE, Choice<WAVES, HERE ? MINE : 1>, int>;
+    // Bounds of 16 blocks per wavefront, afterwards what the choice shares.  A decode step's rows share no blocks: whole rows of bounds go straight into
+    // LDS, past the caches, those of the next blocks under the products of these.  (Loads in the operands' layout touch 16 lines each: 32 long
+    // documents 54.6 us so, through LDS 48.8, and past the caches 44.6; rows of chunks read bounds again and gain nothing, 49.6 and 49.3;
+    // sets of fp32 of 128 are more than LDS holds for enough wavefronts.)
+    constexpr int kRecord = 2 * D * int(sizeof(T)), kSet = 16 * kRecord, kChunks = kRecord / 16, kLoads = kSet / 1024;
+    constexpr bool STAGED = GROUPS == 1 && kRecord <= 512;  // with GROUPS == 1 chunks have rows of 1024 bytes
+    constexpr int kStage = STAGED ? WAVES * kSet : 0;
+    __shared__ __attribute__((aligned(1024))) unsigned char s_stage[kStage > int(sizeof(Chosen)) ? kStage : sizeof(Chosen)];
+    Chosen &s_choice = *reinterpret_cast<Chosen *>(s_stage);
     __shared__ float s_scores[HERE ? THREADS * MINE : 1];
     __shared__ float s_whole_size;
     __shared__ int s_last;
@@ -533,15 +550,46 @@ __global__ __launch_bounds__(THREADS) void block_scores_kernel(const T *__restri
             }
             int b0 = first + 16 * wave;
             int block = b0 < last ? table[min(b0 + r, last - 1)] : 0;
+            // chunk c of row R of a stage lies at c ^ R: 16 rows' chunks of one index fall into 16 places of 256 bytes
+            unsigned char *const stage = s_stage + (STAGED ? wave * kSet : 0);
+            const uint32_t lds = uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(reinterpret_cast<uintptr_t>(stage)))));
+            auto issue = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int row = i * (64 / kChunks) + lane / kChunks, from = __shfl(block, row);
+                    load_to_lds<false>(reinterpret_cast<const unsigned char *>(bounds) + (int64_t(from) * a.num_kv_heads + kvh) * kRecord +
+                                          ((lane % kChunks ^ row) << 4), lds + 1024 * i);
+                }
+            };
+            if (STAGED && b0 < last) {
+                issue();
+                block = table[min(b0 + 16 * WAVES + r, last - 1)];
+            }
             for (; b0 < last; b0 += 16 * WAVES) {
                 const T *src = bounds + (int64_t(block) * a.num_kv_heads + kvh) * 2 * D + 8 * quad;
                 Op lo[J], hi[J];
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    lo[j].load(src + 32 * j);
-                    hi[j].load(src + D + 32 * j);
+                    if constexpr (STAGED) {
+                        if (j == 0) wait_for_loads<0>();
+                        const unsigned char *const row = stage + r * kRecord;
+                        auto place = [&](int c) __attribute__((always_inline)) { return (c ^ r) << 4; };
+                        lo[j].load(row, 8 * quad + 32 * j, place);
+                        hi[j].load(row, 8 * quad + 32 * j + D, place);
+                    } else {
+                        lo[j].load(src + 32 * j);
+                        hi[j].load(src + D + 32 * j);
+                    }
                 }
-                block = table[min(b0 + 16 * WAVES + r, last - 1)];
+                if constexpr (STAGED) {
+                    wait_for_lds();
+                    if (b0 + 16 * WAVES < last) {
+                        issue();
+                        block = table[min(b0 + 32 * WAVES + r, last - 1)];
+                    }
+                } else {
+                    block = table[min(b0 + 16 * WAVES + r, last - 1)];
+                }
                 floatx4 s[GROUPS], up[GROUPS], down[GROUPS];
 #pragma unroll
                 for (int g = 0; g < GROUPS; ++g) s[g] = up[g] = down[g] = floatx4{0.f, 0.f, 0.f, 0.f};

@@ -68,3 +68,21 @@ def test_tiles_are_waited_for_before_they_are_read(tmp_path):
             inside = [ln for ln in body[k_reads[0]:last] if ln.startswith("s_waitcnt") and "vmcnt" in ln]
             ours = {f"vmcnt({loads})", "vmcnt(0)"}
             assert all(any(o in w for o in ours) for w in inside) and sum("vmcnt(0)" in w for w in inside) <= 1, (kernel, inside)
+
+
+def test_bounds_are_waited_for_before_they_are_read(tmp_path):
+    """The loop that takes bounds from a stage in LDS waits for all loads first, and has read all before the next set is asked for."""
+    staged = 0
+    for kernel, body in _kernels(tmp_path, "block_select.hip", "block_scores_kernel").items():
+        loads = [i for i, ln in enumerate(body) if ln.startswith("global_load_lds_dwordx4")]
+        if not loads:
+            continue
+        staged += 1
+        reads = [i for i in range(loads[0], loads[-1]) if body[i].startswith("ds_read_b128")]
+        assert reads, kernel
+        before = [ln for ln in body[loads[0]:reads[0]] if ln.startswith("s_waitcnt") and "vmcnt(0)" in ln]
+        again = next(i for i in loads if i > reads[0])
+        done = [i for i in range(reads[0], again) if body[i].startswith("s_waitcnt") and "lgkmcnt(0)" in body[i]]
+        assert before and done and max(r for r in reads if r < again) < max(done), kernel
+        assert not [r for r in reads if again < r < loads[-1]], kernel
+    assert staged >= 8
