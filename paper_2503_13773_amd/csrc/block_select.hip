@@ -25,7 +25,7 @@
 // Bound: the bounds' bytes in a decode batch, read in pieces of 2 * D * e (32 long documents, 64 / 8 heads of 128, 172 MB:
 // 44.6 us = 3.85 TB/s); the chain of dependent phases where there are few rows (one document of 30 011 tokens:
 // 10.8 us, of which the choice is 4.5); products and LDS for chunks, whose rows share the bounds (1000 rows, 16 / 4 heads of 64 in fp32:
-// 34 us of scores, 13 us of choice).
+// 36 us of scores, 14 us of choice).
 #include <type_traits>
 
 #include "cache_rows.h"
